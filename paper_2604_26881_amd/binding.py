@@ -21,7 +21,8 @@ SYMBOLS = ["moe_status_string", "moe_build_id", "moe_route", "moe_route_segments
            "moe_shared_forward", "moe_shared_forward_ex", "moe_combine", "moe_combine_parts",
            "moe_fused_shared_sets", "moe_fused_workspace_bytes", "moe_expert_group_forward_fused",
            "moe_permute_workspace_bytes", "moe_expert_workspace_bytes", "moe_shared_workspace_bytes",
-           "moe_workspace_bytes", "moe_layer_forward", "moe_layer_shared_sets", "moe_residual_norm", "moe_probe_mfma", "moe_tile_clock_buffer"]
+           "moe_workspace_bytes", "moe_layer_forward", "moe_layer_shared_sets", "moe_residual_norm", "moe_probe_mfma", "moe_tile_clock_buffer",
+           "moe_quantize_mx", "moe_residual_norm_mx", "moe_route_scored", "moe_expert_group_forward_mx"]
 
 
 REFUSALS = (-1, -2, -3)     # MOE_ERR_NULL, MOE_ERR_SHAPE, MOE_ERR_WORKSPACE: the call does not take these arguments
@@ -109,6 +110,16 @@ def load() -> ctypes.CDLL:
     lib.moe_tile_clock_buffer.argtypes = [c_vp, c_int]
     lib.moe_probe_mfma.restype = c_int
     lib.moe_probe_mfma.argtypes = [c_vp, c_sz, c_int, c_int, c_vp, c_vp]
+    c_f = ctypes.c_float
+    lib.moe_quantize_mx.restype = c_int
+    lib.moe_quantize_mx.argtypes = [c_vp, c_int, c_int, c_vp, c_vp, c_vp]
+    lib.moe_residual_norm_mx.restype = c_int
+    lib.moe_residual_norm_mx.argtypes = [c_vp, c_vp, c_vp, c_int, c_int, c_f, c_vp, c_vp, c_vp, c_vp, c_vp]
+    lib.moe_route_scored.restype = c_int
+    lib.moe_route_scored.argtypes = [c_vp] * 3 + [c_int] * 9 + [c_f, c_vp, c_vp, c_vp]
+    lib.moe_expert_group_forward_mx.restype = c_int
+    lib.moe_expert_group_forward_mx.argtypes = ([c_int, c_int, c_vp, c_vp, c_vp, c_int] + [c_vp] * 7 + [c_int] * 4 +
+                                                [c_vp, c_vp, c_sz, c_vp])
     lib.moe_workspace_bytes.restype = c_sz
     lib.moe_workspace_bytes.argtypes = [c_int] * 6
     _LIB = lib
@@ -406,6 +417,124 @@ def moe_residual_norm(x, y, out=None, eps: float = 1e-6):
                                   _ptr(out, torch.bfloat16, "out"), _stream())
     _check(rc, "moe_residual_norm")
     return out
+
+
+def _here(what: str, **tensors) -> None:
+    """All given tensors on the current device, whose stream the call takes."""
+    for name, t in tensors.items():
+        if t is not None and (not t.is_cuda or t.device.index != torch.cuda.current_device()):
+            raise MoeError(f"{what}: {name} must be on the current GPU, it is on {t.device}")
+
+
+def _mx(pair, shape, name: str, what: str):
+    """Addresses of an 8-bit tensor's values (of the given shape) and scales."""
+    q, scales = pair
+    if tuple(q.shape) != tuple(shape) or tuple(scales.shape) != (*shape[:-1], shape[-1] // 32):
+        raise MoeError(f"{what}: {name} must be values {tuple(shape)} with scales {(*shape[:-1], shape[-1] // 32)}, "
+                       f"got {tuple(q.shape)} and {tuple(scales.shape)}")
+    _here(what, **{name: q, f"{name} scales": scales})
+    return _ptr(q, torch.float8_e4m3fn, name), _ptr(scales, torch.float8_e8m0fnu, f"{name} scales")
+
+
+def _as(t, shape, name: str, what: str):
+    if t is not None and tuple(t.shape) != tuple(shape):
+        raise MoeError(f"{what}: {name} must be {tuple(shape)}, got {tuple(t.shape)}")
+    return t
+
+
+def moe_quantize_mx(x, q=None, scales=None):
+    """bf16 x [.., H] as 8-bit values: (q [.., H] float8_e4m3fn, scales [.., H / 32] float8_e8m0fnu), one scale per 32
+    neighbours of the last dimension."""
+    H = x.shape[-1]
+    if H % 64 != 0 or H == 0:
+        raise MoeError(f"moe_quantize_mx: the last dimension must be a multiple of 64, got {H}")
+    _here("moe_quantize_mx", x=x)
+    if q is None:
+        q = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=x.device)
+    if scales is None:
+        scales = torch.empty((*x.shape[:-1], H // 32), dtype=torch.float8_e8m0fnu, device=x.device)
+    q_p, s_p = _mx((q, scales), x.shape, "q", "moe_quantize_mx")
+    rc = load().moe_quantize_mx(_ptr(x, torch.bfloat16, "x"), x.numel() // H, H, q_p, s_p, _stream())
+    _check(rc, "moe_quantize_mx")
+    return q, scales
+
+
+def moe_residual_norm_mx(x, y=None, weight=None, eps: float = 1e-6, sum=None, out=None, q=None, scales=None,
+                         keep_sum: bool = True, keep_out: bool = True, quantize: bool = True):
+    """u = x + y (y None: x); n = u / sqrt(mean(u^2) + eps) * weight.  Returns (sum = bf16(u), out = bf16(n), q, scales = n in
+    8 bits), None for what is not wanted.  sum and out may be x or y."""
+    what = "moe_residual_norm_mx"
+    T, H = x.shape
+    if H % 64 != 0:
+        raise MoeError(f"{what}: H must be a multiple of 64, got {H}")
+    _as(y, (T, H), "y", what), _as(weight, (H,), "weight", what)
+    _here(what, x=x, y=y, weight=weight, sum=sum, out=out)
+    sum = (torch.empty_like(x) if sum is None else _as(sum, (T, H), "sum", what)) if keep_sum else None
+    out = (torch.empty_like(x) if out is None else _as(out, (T, H), "out", what)) if keep_out else None
+    q_p = s_p = None
+    if quantize:
+        q = torch.empty((T, H), dtype=torch.float8_e4m3fn, device=x.device) if q is None else q
+        scales = torch.empty((T, H // 32), dtype=torch.float8_e8m0fnu, device=x.device) if scales is None else scales
+        q_p, s_p = _mx((q, scales), (T, H), "q", what)
+    else:
+        q = scales = None
+    bf = torch.bfloat16
+    rc = load().moe_residual_norm_mx(_ptr(x, bf, "x"), _ptr(y, bf, "y"), _ptr(weight, bf, "weight"), T, H, float(eps),
+                                     _ptr(sum, bf, "sum"), _ptr(out, bf, "out"), q_p, s_p, _stream())
+    _check(rc, what)
+    return sum, out, q, scales
+
+
+SCORES = {"softmax": 0, "sigmoid": 1}
+
+
+def moe_route_scored(x, Wr, balance, K: int, score: str = "softmax", groups: int = 1, top_groups: int = 1, group_best: int = 1,
+                     renorm: bool = False, scale: float = 1.0, topk_ids=None, topk_w=None):
+    """Gating by scores ("softmax" or "sigmoid" of the router logits): the choice compares score + balance (balance [E] fp32 or
+    None), among the top_groups of `groups` equal groups whose best (group_best 1) or two best (2) sum to the most; the
+    weights are the scores, divided by their sum with renorm, times scale."""
+    what = "moe_route_scored"
+    if score not in SCORES:
+        raise MoeError(f"{what}: score must be one of {sorted(SCORES)}, got {score!r}")
+    T, H = x.shape
+    E = Wr.shape[0]
+    _as(Wr, (E, H), "Wr", what), _as(balance, (E,), "balance", what)
+    _as(topk_ids, (T, K), "topk_ids", what), _as(topk_w, (T, K), "topk_w", what)
+    _here(what, x=x, Wr=Wr, balance=balance, topk_ids=topk_ids, topk_w=topk_w)
+    if topk_ids is None:
+        topk_ids = torch.empty((T, K), dtype=torch.int32, device=x.device)
+    if topk_w is None:
+        topk_w = torch.empty((T, K), dtype=torch.float32, device=x.device)
+    rc = load().moe_route_scored(_ptr(x, torch.bfloat16, "x"), _ptr(Wr, torch.bfloat16, "Wr"), _ptr(balance, torch.float32, "balance"),
+                                 T, H, E, int(K), SCORES[score], int(groups), int(top_groups), int(group_best), int(bool(renorm)),
+                                 float(scale), _ptr(topk_ids, torch.int32, "topk_ids"), _ptr(topk_w, torch.float32, "topk_w"),
+                                 _stream())
+    _check(rc, what)
+    return topk_ids, topk_w
+
+
+def moe_expert_group_forward_mx(group_lo: int, group_hi: int, x, src_of_row, K: int, expert_offsets, Wg, Wu, Wd, Yp, workspace=None):
+    """The block invocation on 8-bit rows and weights: x, Wg, Wu, Wd are (values, scales) pairs as moe_quantize_mx makes them.
+    src_of_row None: x is the permuted copy [P,H]; otherwise row r of the batch is x[src_of_row[r] // K]."""
+    what = "moe_expert_group_forward_mx"
+    E, I, H = Wg[0].shape
+    P = Yp.shape[0]
+    if src_of_row is not None and (K < 1 or src_of_row.numel() != P or x[0].shape[0] * K != P):
+        raise MoeError(f"{what}: x must have P / K rows and src_of_row P entries")
+    if expert_offsets.numel() != E + 1:
+        raise MoeError(f"{what}: expert_offsets must have E + 1 entries")
+    _as(Yp, (P, H), "Yp", what)
+    x_p = _mx(x, (P if src_of_row is None else P // K, H), "x", what)
+    w_p = [a for name, w, n, k in (("Wg", Wg, I, H), ("Wu", Wu, I, H), ("Wd", Wd, H, I)) for a in _mx(w, (E, n, k), name, what)]
+    if workspace is None:
+        workspace = torch.empty(max(int(load().moe_expert_workspace_bytes(P, I)), 256), dtype=torch.uint8, device=Yp.device)
+    _here(what, src_of_row=src_of_row, expert_offsets=expert_offsets, Yp=Yp, workspace=workspace)
+    rc = load().moe_expert_group_forward_mx(int(group_lo), int(group_hi), *x_p, _ptr(src_of_row, torch.int32, "src_of_row"), int(K),
+                                            _ptr(expert_offsets, torch.int32, "expert_offsets"), *w_p, P, H, E, I,
+                                            _ptr(Yp, torch.bfloat16, "Yp"), _ptr(workspace, None, "workspace"),
+                                            workspace.numel() * workspace.element_size(), _stream())
+    _check(rc, what)
+    return Yp
 
 
 @dataclass

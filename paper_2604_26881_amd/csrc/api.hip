@@ -5,6 +5,7 @@
 #include "../../include/moe.h"
 #include "../../include/moe_tuning.h"
 #include "common.h"
+#include "mx.h"
 
 using namespace moe;
 
@@ -650,6 +651,72 @@ int moe_residual_norm(const void* x, const void* y, int T, int H, float eps, voi
   if (T == 0) return MOE_OK;
   if (!x || !y || !out) return MOE_ERR_NULL;
   return launch_residual_norm(x, y, T, H, eps, out, (hipStream_t)stream);
+}
+
+// ---- 8-bit rows and weights
+
+static bool aligned(const void* p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
+
+int moe_quantize_mx(const void* x, int rows, int H, void* q, void* scales, void* stream) {
+  if (rows < 0 || !dims_ok(H)) return MOE_ERR_SHAPE;
+  if (rows == 0) return MOE_OK;
+  if (!x || !q || !scales) return MOE_ERR_NULL;
+  if (!aligned(x, 16) || !aligned(q, 16) || !aligned(scales, 2)) return MOE_ERR_SHAPE;
+  return launch_quantize_mx(x, rows, H, q, scales, (hipStream_t)stream);
+}
+
+int moe_residual_norm_mx(const void* x, const void* y, const void* weight, int T, int H, float eps, void* sum, void* out, void* q,
+                         void* scales, void* stream) {
+  if (T < 0 || !dims_ok(H) || H > 8192 || !(eps >= 0.0f)) return MOE_ERR_SHAPE;
+  if (T == 0) return MOE_OK;
+  if (!x || (q == nullptr) != (scales == nullptr) || (!sum && !out && !q)) return MOE_ERR_NULL;
+  if (!aligned(x, 16) || !aligned(y, 16) || !aligned(weight, 16) || !aligned(sum, 16) || !aligned(out, 16) || !aligned(q, 16) ||
+      !aligned(scales, 2))
+    return MOE_ERR_SHAPE;
+  return launch_residual_norm_mx(x, y, weight, T, H, eps, sum, out, q, scales, (hipStream_t)stream);
+}
+
+int moe_route_scored(const void* x, const void* Wr, const float* balance, int T, int H, int E, int K, int score, int n_groups,
+                     int top_groups, int group_best, int renorm, float scale, int32_t* topk_ids, float* topk_w, void* stream) {
+  if (T < 0 || !dims_ok(H) || H > 8192 || E < 1 || E > 256 || K < 1 || K > 16 || K > E) return MOE_ERR_SHAPE;
+  if (score != MOE_SCORE_SOFTMAX && score != MOE_SCORE_SIGMOID) return MOE_ERR_SHAPE;
+  if (n_groups < 1 || n_groups > 64 || E % n_groups != 0 || top_groups < 1 || top_groups > n_groups || K > top_groups * (E / n_groups))
+    return MOE_ERR_SHAPE;
+  if (group_best < 1 || group_best > 2 || group_best > E / n_groups || !(scale - scale == 0.0f)) return MOE_ERR_SHAPE;
+  if (T == 0) return MOE_OK;
+  if (!x || !Wr || !topk_ids || !topk_w) return MOE_ERR_NULL;
+  if (!aligned(x, 16) || !aligned(Wr, 16)) return MOE_ERR_SHAPE;
+  return launch_route_scored(RouteScored{(const bf16_t*)x, (const bf16_t*)Wr, balance, T, H, E, K, score == MOE_SCORE_SIGMOID, n_groups,
+                                         top_groups, group_best, renorm, scale, topk_ids, topk_w}, (hipStream_t)stream);
+}
+
+int moe_expert_group_forward_mx(int group_lo, int group_hi, const void* x, const void* x_scales, const int32_t* src_of_row, int K,
+                                const int32_t* expert_offsets, const void* Wg, const void* Wg_scales, const void* Wu,
+                                const void* Wu_scales, const void* Wd, const void* Wd_scales, int P, int H, int E, int I,
+                                void* Yp, void* workspace, size_t workspace_bytes, void* stream) {
+  if (P < 0 || !dims_ok(H) || !dims_ok(I) || H > MX_DIM_MAX || I > MX_DIM_MAX || E < 1 || E > 256) return MOE_ERR_SHAPE;
+  if (group_lo < 0 || group_hi > E || group_lo >= group_hi) return MOE_ERR_SHAPE;
+  if ((long long)P * (H > I ? H : I) >= (1ll << 31)) return MOE_ERR_SHAPE;
+  if (src_of_row != nullptr && (K < 1 || K > 16 || P % K != 0)) return MOE_ERR_SHAPE;
+  if (P == 0) return MOE_OK;
+  if (!x || !x_scales || !expert_offsets || !Wg || !Wg_scales || !Wu || !Wu_scales || !Wd || !Wd_scales || !Yp || !workspace)
+    return MOE_ERR_NULL;
+  for (const void* p : {x, Wg, Wg_scales, Wu, Wu_scales, Wd, Wd_scales, (const void*)Yp, (const void*)workspace})
+    if (!aligned(p, 16)) return MOE_ERR_SHAPE;
+  if (!aligned(x_scales, 2)) return MOE_ERR_SHAPE;
+  if (workspace_bytes < (size_t)P * (size_t)I * 2) return MOE_ERR_WORKSPACE;   // h, bf16 [P,I]
+  MxArgs gu{};
+  gu.A = (const uint8_t*)x; gu.As = (const uint8_t*)x_scales;
+  gu.B0 = (const uint8_t*)Wg; gu.B0s = (const uint8_t*)Wg_scales; gu.B1 = (const uint8_t*)Wu; gu.B1s = (const uint8_t*)Wu_scales;
+  gu.C = (bf16_t*)workspace;
+  gu.offsets = expert_offsets; gu.lo = group_lo; gu.hi = group_hi; gu.rows_total = P; gu.mean_rows = (P + E - 1) / E;
+  gu.N = I; gu.Kdim = H;
+  MxArgs dn = gu;
+  gu.gather = src_of_row; gu.gather_div = src_of_row ? K : 1;
+  dn.A = (const uint8_t*)workspace; dn.As = nullptr; dn.B0 = (const uint8_t*)Wd; dn.B0s = (const uint8_t*)Wd_scales; dn.B1 = dn.B1s = nullptr;
+  dn.C = (bf16_t*)Yp; dn.N = H; dn.Kdim = I;
+  const int rc = launch_stream_mx_gateup(gu, (hipStream_t)stream);
+  return rc != 0 ? rc : launch_stream_mx_down(dn, (hipStream_t)stream);
 }
 
 }  // extern "C"

@@ -1,0 +1,107 @@
+// Rows of bf16 to 8-bit rows with scales, alone and behind the residual norm that precedes an MoE layer.
+//
+// Both are streams: every input is read once, every output written once, the row stays in registers in between.  A lane
+// holds 8 neighbours (one 16-byte load, one 8-byte store), so the 32 values of a scale are the four lanes of a quad and
+// their maximum is two lane exchanges.
+#include "mx.h"
+
+namespace moe {
+
+// Eight values of this lane, a quarter of a block: their bytes to q[0 .. 8), the scale by the quad's first lane to *scale
+__device__ __forceinline__ void store_mx8(const float (&v)[8], uint8_t* __restrict__ q, uint8_t* __restrict__ scale) {
+  uint32_t a = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) a = max(a, magnitude(v[i]));
+  const uint32_t byte = mx_scale_byte(quad_max(a));
+  const float inv = mx_inverse(byte);
+  uint2 o;
+  o.x = mx_pack4(v[0], v[1], v[2], v[3], inv, byte);
+  o.y = mx_pack4(v[4], v[5], v[6], v[7], inv, byte);
+  *reinterpret_cast<uint2*>(q) = o;
+  if ((threadIdx.x & 3) == 0) *scale = (uint8_t)byte;
+}
+__device__ __forceinline__ void widen(u32x4 v, float (&f)[8]) {
+  f[0] = bf16_lo(v.x); f[1] = bf16_hi(v.x); f[2] = bf16_lo(v.y); f[3] = bf16_hi(v.y);
+  f[4] = bf16_lo(v.z); f[5] = bf16_hi(v.z); f[6] = bf16_lo(v.w); f[7] = bf16_hi(v.w);
+}
+
+// n8: eighths, rows * H / 8 (the rows are contiguous, and H is whole blocks)
+__global__ __launch_bounds__(256) void quantize_mx_kernel(const bf16_t* __restrict__ x, size_t n8, uint8_t* __restrict__ q,
+                                                          uint8_t* __restrict__ scales) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n8) return;     // (n8 is a multiple of 8: quads leave together)
+  float v[8];
+  widen(reinterpret_cast<const u32x4*>(x)[i], v);
+  store_mx8(v, q + 8 * i, scales + i / 4);
+}
+
+int launch_quantize_mx(const void* x, int rows, int H, void* q, void* scales, hipStream_t st) {
+  const size_t n8 = (size_t)rows * (size_t)(H / 8);
+  const size_t groups = (n8 + 255) / 256;
+  if (groups == 0) return 0;
+  if (groups > 0x7fffffffull) return -2;
+  hipLaunchKernelGGL(quantize_mx_kernel, dim3((unsigned)groups), dim3(256), 0, st, (const bf16_t*)x, n8, (uint8_t*)q, (uint8_t*)scales);
+  return hipGetLastError() == hipSuccess ? 0 : -4;
+}
+
+// u = x + y; n = u / sqrt(mean(u^2) + eps) * weight.  One workgroup per token row, up to 4 x 8 values per lane (H <= 8192);
+// sums of squares in fp32.  sum and out are rounded once from fp32, and so are the 8-bit rows (from n itself, not from out).
+__global__ __launch_bounds__(256) void residual_norm_mx_kernel(const bf16_t* x, const bf16_t* y, const bf16_t* __restrict__ weight,
+                                                               int H, float eps, bf16_t* sum, bf16_t* out,
+                                                               uint8_t* __restrict__ q, uint8_t* __restrict__ scales) {
+  const size_t t = blockIdx.x;
+  __shared__ float s_part[4];
+  float u[4][8];
+  float ss = 0.0f;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int c = threadIdx.x + 256 * r;
+    if (c < H / 8) {
+      widen(reinterpret_cast<const u32x4*>(x + t * H)[c], u[r]);
+      if (y != nullptr) {
+        float v[8];
+        widen(reinterpret_cast<const u32x4*>(y + t * H)[c], v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u[r][i] += v[i];
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) ss = __builtin_fmaf(u[r][i], u[r][i], ss);
+    }
+  }
+  ss = wave_sum(ss);
+  if ((threadIdx.x & 63) == 0) s_part[threadIdx.x >> 6] = ss;
+  __syncthreads();
+  const float scale = 1.0f / sqrtf(((s_part[0] + s_part[1]) + (s_part[2] + s_part[3])) / (float)H + eps);
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int c = threadIdx.x + 256 * r;
+    if (c < H / 8) {
+      if (sum != nullptr)
+        reinterpret_cast<u32x4*>(sum + t * H)[c] = u32x4{pack_bf16x2(u[r][0], u[r][1]), pack_bf16x2(u[r][2], u[r][3]),
+                                                         pack_bf16x2(u[r][4], u[r][5]), pack_bf16x2(u[r][6], u[r][7])};
+      float n[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) n[i] = u[r][i] * scale;
+      if (weight != nullptr) {
+        float v[8];
+        widen(reinterpret_cast<const u32x4*>(weight)[c], v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) n[i] *= v[i];
+      }
+      if (out != nullptr)
+        reinterpret_cast<u32x4*>(out + t * H)[c] = u32x4{pack_bf16x2(n[0], n[1]), pack_bf16x2(n[2], n[3]),
+                                                         pack_bf16x2(n[4], n[5]), pack_bf16x2(n[6], n[7])};
+      if (q != nullptr) store_mx8(n, q + t * H + 8 * c, scales + t * (H / MX) + c / 4);
+    }
+  }
+}
+
+int launch_residual_norm_mx(const void* x, const void* y, const void* weight, int T, int H, float eps, void* sum, void* out,
+                            void* q, void* scales, hipStream_t st) {
+  if (T == 0) return 0;
+  hipLaunchKernelGGL(residual_norm_mx_kernel, dim3(T), dim3(256), 0, st, (const bf16_t*)x, (const bf16_t*)y, (const bf16_t*)weight, H,
+                     eps, (bf16_t*)sum, (bf16_t*)out, (uint8_t*)q, (uint8_t*)scales);
+  return hipGetLastError() == hipSuccess ? 0 : -4;
+}
+
+}  // namespace moe

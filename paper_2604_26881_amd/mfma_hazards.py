@@ -26,9 +26,10 @@ from __future__ import annotations
 import re
 from typing import Dict, Iterator, List, Optional, Tuple
 
-# wait states between an MFMA and a non-MFMA instruction touching its result, by output shape of the bf16
-# instructions this library uses (32x32x16: 8 passes, 16x16x32: 4 passes); anything else: the largest value
-_WAIT_STATES = {"v_mfma_f32_32x32x16_bf16": 11, "v_mfma_f32_16x16x32_bf16": 7}
+# wait states between an MFMA and a non-MFMA instruction touching its result, by output shape of the instructions this
+# library uses (bf16 32x32x16: 8 passes, 16x16x32: 4; 8-bit values 16x16x128: 8, 32x32x64: 16); anything else: the largest
+_WAIT_STATES = {"v_mfma_f32_32x32x16_bf16": 11, "v_mfma_f32_16x16x32_bf16": 7, "v_mfma_scale_f32_16x16x128_f8f6f4": 11,
+                "v_mfma_scale_f32_32x32x64_f8f6f4": 19}
 _DEFAULT_WAIT_STATES = 19
 _REG = re.compile(r"\b([va])(?:(\d+)|\[(\d+):(\d+)\])")
 
