@@ -17,7 +17,7 @@ CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libmoe_hip.so")
 OBJDIR = os.path.join(HERE, "_build")
 SOURCES = ["api.hip", "route.hip", "permute.hip", "combine.hip", "expert_tile.hip", "expert_stream_lds.hip", "expert_stream_wide.hip", "mfma_probe.hip",
-           "rows_mx.hip", "route_scored.hip", "expert_stream_mx.hip"]
+           "rows_mx.hip", "route_scored.hip", "expert_stream_mx.hip", "expert_tile_mx.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          # the global->LDS copy sets m0 itself (the instruction takes its LDS address from there); the compiler

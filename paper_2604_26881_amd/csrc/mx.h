@@ -64,6 +64,8 @@ struct MxArgs {
 };
 int launch_stream_mx_gateup(const MxArgs& a, hipStream_t st);
 int launch_stream_mx_down(const MxArgs& a, hipStream_t st);
+int launch_tile_mx_gateup(const MxArgs& a, hipStream_t st);
+int launch_tile_mx_down(const MxArgs& a, hipStream_t st);
 
 int launch_quantize_mx(const void* x, int rows, int H, void* q, void* scales, hipStream_t st);
 int launch_residual_norm_mx(const void* x, const void* y, const void* weight, int T, int H, float eps, void* sum, void* out,

@@ -263,6 +263,7 @@ def check_block(c, Yp):
 COUNTS = [  # rows per expert (names the kernels by their mean), H, I
     ([1], 64, 64), ([1, 0, 0, 2], 64, 128), ([0, 3, 1, 0, 16, 17, 5, 2], 192, 320), ([1, 2, 1, 0, 4], 2048, 1408), ([15, 16, 17, 33, 0, 1], 448, 576),
     ([31, 32, 33, 64, 65, 1], 256, 192), ([40, 63, 100, 129, 1, 0, 7], 320, 448), ([128, 127, 300, 1, 0, 255, 256, 257], 512, 384),
+    ([100, 60, 128, 129, 0, 65, 200, 31], 384, 320), ([100, 60, 128, 129, 0, 65, 200, 31], 448, 192), ([33, 40, 64, 63, 65, 1, 0, 50], 256, 256),
     ([700, 90], 1088, 704), ([513], 192, 256), ([2, 3], 16384, 64), ([3, 2], 64, 16384),
 ]
 
