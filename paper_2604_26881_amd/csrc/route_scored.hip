@@ -1,169 +1,571 @@
 // Gating by scores: softmax or sigmoid of the router logits, an optional bias that takes part in the choice alone, experts
 // in groups of which only the best are considered, top-k, renormalised and scaled weights.
 //
-//   l[t,e] = <x[t,:], Wr[e,:]>   in the order of additions of route.hip, so both calls see the same logits
+//   l[t,e] = <x[t,:], Wr[e,:]>   in the order of additions of route.hip, so both calls choose from the same logits
 //   s[t,e] = softmax_e(l) or sigmoid(l), formed in 64 bits and rounded once to fp32;   c = s + balance
 //   value of a group = its largest c, or the sum of its two largest;  the top_groups best groups are kept
 //   ids = the K largest c among the kept groups' experts;  w = s[id] (over their sum + 1e-20 with renorm) * scale
-//
-// Why 64 bits: the choice compares scores, and a score's last bit would otherwise be the library exponential's business.
-// With the rounding of an exact value, every implementation of the formula chooses alike.
 // NaN orders below everything, so the ids are K different experts whatever the rows hold.
+//
+// What bounds it: the products.  In the defined order they are one vector multiply-add each; on the matrix cores they are almost free,
+// but add up in another order, and ids must not depend on that.  So: logits from the matrix cores with a bound of their
+// error, the choice from those; and where two candidates lie closer than the bound allows, the logits of just these are formed
+// again in the defined order (and their scores in 64 bits) and the choice is repeated: an id is always the definition's.
+// (Weights come from the logits at hand, whose last bits are either evaluation's.)  About one token in forty is looked at
+// twice (256 experts in 8 groups, H 2048).
+//
+// The bound: one 16x16x32 step is off by at most 6 * 2^-24 of the sum of its terms' magnitudes (measured, products over 18
+// orders of magnitude among them), whole logits of H 2048 by 1.3 * 2^-24 of theirs, and the defined order by less; assumed
+// are 32 * 2^-24 (beyond H 2048 H / 64 * 2^-24) of |x[t]| * max_e |Wr[e]|, which is more than that sum.
 #include "fold.h"
 #include "mx.h"
+#include <type_traits>
 
 namespace moe {
+namespace {
 
-constexpr int SCORED_EMAX = 256;
+constexpr float LOGIT_ERROR = 32.0f / 16777216.0f;
 
-__device__ __forceinline__ uint32_t fold_umax(uint32_t a) {
-  auto step = [&](auto ctrl, auto rmask) {
-    a = max(a, (uint32_t)__builtin_amdgcn_update_dpp((int)a, (int)a, decltype(ctrl)::value, decltype(rmask)::value, 0xF, false));
-  };
-  step(std::integral_constant<int, 0xB1>{}, std::integral_constant<int, 0xF>{});
-  step(std::integral_constant<int, 0x4E>{}, std::integral_constant<int, 0xF>{});
-  step(std::integral_constant<int, 0x141>{}, std::integral_constant<int, 0xF>{});
-  step(std::integral_constant<int, 0x140>{}, std::integral_constant<int, 0xF>{});
-  step(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xA>{});
-  step(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xC>{});
-  return (uint32_t)__builtin_amdgcn_readlane((int)a, 63);
-}
-// Whole numbers that order like the values: -0 as +0, NaN as 0, below -infinity
+// Whole numbers that order like the values: -0 as +0, NaN as 1, below -infinity; 0 is left for "no expert"
 __device__ __forceinline__ uint32_t order_key(float v) {
   const uint32_t b = __float_as_uint(v + 0.0f);
-  return v != v ? 0u : (b >> 31) ? ~b : b | 0x80000000u;
+  return v != v ? 1u : (b >> 31) ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float key_value(uint32_t k) {
-  return k == 0u ? __uint_as_float(0x7fc00000u) : __uint_as_float((k >> 31) ? k & 0x7fffffffu : ~k);
+  return k <= 1u ? __uint_as_float(0x7fc00000u) : __uint_as_float((k >> 31) ? k & 0x7fffffffu : ~k);
+}
+__device__ __forceinline__ double sigmoid64(float l) { return 1.0 / (1.0 + exp(-(double)l)); }
+
+// Folds over a row of 16 lanes; every lane has the result
+template <class T, class F>
+__device__ __forceinline__ T row_fold(T v, F&& f) {
+  auto other = [](T x, auto ctrl) {
+    return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xF, 0xF, false));
+  };
+  v = f(v, other(v, std::integral_constant<int, 0xB1>{}));
+  v = f(v, other(v, std::integral_constant<int, 0x4E>{}));
+  v = f(v, other(v, std::integral_constant<int, 0x141>{}));
+  return f(v, other(v, std::integral_constant<int, 0x140>{}));
+}
+__device__ __forceinline__ uint32_t row_max(uint32_t v) { return row_fold(v, [](uint32_t a, uint32_t b) { return max(a, b); }); }
+__device__ __forceinline__ uint32_t row_min(uint32_t v) { return row_fold(v, [](uint32_t a, uint32_t b) { return min(a, b); }); }
+__device__ __forceinline__ float row_max(float v) { return row_fold(v, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ __forceinline__ float row_sum(float v) { return row_fold(v, [](float a, float b) { return a + b; }); }
+
+// N logits by one wave, of token rows x[n] (or one for all) and router rows w[n], in the defined order.  Four chunks of 512 at a time
+// are requested before they are used.
+template <int NX, int N>
+__device__ __forceinline__ void defined_logits(const bf16_t* const (&x)[NX], const bf16_t* const (&w)[N], int H, int lane, float (&l)[N]) {
+  static_assert(NX == 1 || NX == N, "one row for all, or one each");
+  float acc[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n) acc[n] = 0.0f;
+  for (int h0 = 8 * lane; h0 < H; h0 += 2048) {
+    u32x4 xv[NX][4], wv[N][4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const bool in = h0 + 512 * c < H;      // (a product of zeros leaves a sum as it is)
+#pragma unroll
+      for (int n = 0; n < NX; ++n) xv[n][c] = in ? *reinterpret_cast<const u32x4*>(x[n] + h0 + 512 * c) : u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+      for (int n = 0; n < N; ++n) wv[n][c] = in ? *reinterpret_cast<const u32x4*>(w[n] + h0 + 512 * c) : u32x4{0u, 0u, 0u, 0u};
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        float xf[8], wf[8];
+        widen8(xv[NX == 1 ? 0 : n][c], xf);
+        widen8(wv[n][c], wf);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[n] = __builtin_fmaf(xf[i], wf[i], acc[n]);
+      }
+  }
+#pragma unroll
+  for (int n = 0; n < N; ++n) l[n] = fold_sum(acc[n]);
 }
 
-// Scores of one token by one wave: l[i] is the logit of expert lane + 64 i
-__device__ __forceinline__ void form_scores(const RouteScored& a, const float (&l)[4], int lane, float (&s)[4]) {
-  if (a.sigmoid) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) s[i] = (float)(1.0 / (1.0 + exp(-(double)l[i])));
-    return;
-  }
-  float m = -INFINITY;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (lane + 64 * i < a.E) m = fmaxf(m, l[i]);
-  m = fold_max(m);
-  double p[4], z = 0.0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    p[i] = lane + 64 * i < a.E ? exp((double)l[i] - (double)m) : 0.0;
-    z += p[i];
-  }
-#pragma unroll
-  for (int w = 1; w < 64; w <<= 1) z += __shfl_xor(z, w, WAVE);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) s[i] = (float)(p[i] / z);
-}
+constexpr int GROUPS_MAX = 64;
 
-// Choice and weights of one token by one wave; key[i] and s[i] belong to expert lane + 64 i, s_key holds 256 keys of the wave.
-__device__ __forceinline__ void choose(const RouteScored& a, const uint32_t (&key)[4], const float (&s)[4], int lane,
-                                       uint32_t* s_key, int t) {
-  bool out[4];
+// Four tokens by one wave, one per row of 16 lanes; lane j of a row owns experts EPL j .. EPL j + EPL - 1.  What belongs to a token
+// is the same in the 16 lanes of its row.
+//   t, want: the token and whether its row of results is asked for;  whole: its logits are the defined ones;
+//   s_logit: its logits in LDS (by expert; exact ones are written back);  s_bal: the balance, by expert, at most bal_most;
+//   doubt: what a logit may be off by, negative if that is not known;  s_key, s_thr: EPL * 16 and 64 words of the row.
+// True where the choice cannot be made without all of the token's logits in the defined order; then nothing is written.
+template <int EPL>
+__device__ __forceinline__ bool choose(const RouteScored& a, int t, bool want, bool whole, float* s_logit, const float* s_bal, float bal_most,
+                                       float doubt, int lane, uint32_t* s_key, float* s_thr) {
+  const int j16 = lane & 15, e0 = EPL * j16;
+  const int size = a.E / a.groups;
+  const uint32_t per_group = 65536u / (uint32_t)size + 1u;                   // e / size = e * per_group >> 16 for e < 256
+  const bool grouped = a.groups > a.top_groups;
+  // softmax without extras orders like its logits
+  const bool by_logit = !whole && !a.sigmoid && a.balance == nullptr && (!grouped || a.best == 1);
+  auto row_any = [&](bool v) { return ((__ballot(v) >> (lane & 48)) & 0xffffull) != 0ull; };
+
+  uint32_t key[EPL];         // what is compared, 0 beyond E
+  float m = 0.0f, share = 0.0f;
+  double z = 1.0;
+  unsigned exact = 0u;       // this lane's experts whose logit (and key) is the defined one
+  bool redo = false;
+  {
+    float l[EPL];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) out[i] = lane + 64 * i >= a.E;
-  if (a.groups > a.top_groups) {
-    const int size = a.E / a.groups;
+    for (int i = 0; i < EPL; i += 4) {
+      const f32x4 v = *reinterpret_cast<const f32x4*>(s_logit + e0 + i);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s_key[lane + 64 * i] = key[i];
-    __builtin_amdgcn_wave_barrier();
-    uint32_t k1 = 0, k2 = 0;       // the two largest keys of group `lane`
-    if (lane < a.groups) {
-      for (int j = 0; j < size; ++j) {
-        const uint32_t k = s_key[lane * size + j];
-        k2 = max(k2, min(k1, k));
-        k1 = max(k1, k);
+      for (int j = 0; j < 4; ++j) l[i + j] = e0 + i + j < a.E ? v[j] : 0.0f;
+    }
+    float magnitudes = 0.0f, top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+      magnitudes += fabsf(l[i]);
+      if (e0 + i < a.E) top = fmaxf(top, l[i]);
+    }
+    if (row_any(magnitudes != 0.0f)) redo = !whole && (doubt < 0.0f || row_any(!(magnitudes < INFINITY)));
+    else doubt = 0.0f;       // (a row of zeros: 0 in any order)
+    if (!a.sigmoid) m = row_max(top);
+    if (__any(whole)) {      // scores in 64 bits
+      double sum = 0.0;
+      if (!a.sigmoid) {
+#pragma unroll 1
+        for (int i = 0; i < EPL; ++i)
+          if (e0 + i < a.E) sum += exp((double)s_logit[e0 + i] - (double)m);
+#pragma unroll
+        for (int w = 1; w < 16; w <<= 1) sum += __shfl_xor(sum, w, WAVE);
+      }
+#pragma unroll 1
+      for (int i = 0; i < EPL; ++i) {
+        const double v = (double)s_logit[e0 + i];
+        s_key[e0 + i] = __float_as_uint((float)(a.sigmoid ? 1.0 / (1.0 + exp(-v)) : exp(v - (double)m) / sum));
+      }
+      if (whole) {
+        z = sum;
+        exact = ~0u;
       }
     }
-    const uint32_t value = a.best == 1 ? k1 : order_key(key_value(k1) + key_value(k2));
-    bool left = lane < a.groups;
-    unsigned long long kept = 0ull;
-    for (int j = 0; j < a.top_groups; ++j) {
-      const uint32_t best = fold_umax(left ? value : 0u);
-      const int g = __builtin_ctzll(__ballot(left && value == best));
-      kept |= 1ull << g;
-      if (lane == g) left = false;
+    if (a.sigmoid) {
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) l[i] = whole ? __uint_as_float(s_key[e0 + i]) : __fdividef(1.0f, 1.0f + __expf(-l[i]));
+    } else if (!by_logit) {
+      float sum = 0.0f;
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) {
+        l[i] = whole ? __uint_as_float(s_key[e0 + i]) : e0 + i < a.E ? expf(l[i] - m) : 0.0f;
+        sum += l[i];
+      }
+      sum = row_sum(sum);
+      if (!whole) {
+        z = sum;
+        share = 2.1f * doubt + 4e-6f;
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) l[i] = l[i] / sum;
+      }
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (!out[i]) out[i] = ((kept >> ((lane + 64 * i) / size)) & 1ull) == 0ull;
+    for (int i = 0; i < EPL; ++i) key[i] = e0 + i < a.E ? order_key(a.balance != nullptr ? l[i] + s_bal[e0 + i] : l[i]) : 0u;
   }
+  // what a compared value of magnitude c may be off by
+  const float own = a.sigmoid ? 0.25f * doubt + 2e-6f : by_logit ? doubt : 0.0f, largest = 1.0f / (float)z;
+  auto off = [&](float c) {
+    const float rounded = 2.4e-7f * c;
+    return a.sigmoid || by_logit ? own + rounded : share * fminf(largest, c + bal_most) + rounded + 1e-37f;
+  };
   int my_id = 0;
-  float my_s = 0.0f, run = 0.0f;
-  for (int j = 0; j < a.K; ++j) {
-    uint32_t k = 0;
+  for (;;) {
+    unsigned again = 0u;     // this lane's experts whose logit the choice needs exactly
+    bool alike = false;      // softmax: so close, or so far below the largest, that scores may round alike
+    uint32_t cur[EPL];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (!out[i]) k = max(k, key[i]);
-    k = fold_umax(k);
-    int e = -1;
-    float mine = 0.0f;
+    for (int i = 0; i < EPL; ++i) cur[i] = key[i];
+
+    if (grouped) {
+      // lane j of a row takes groups j, j + 16, ..: their two largest keys, then the best groups one by one
+#pragma unroll
+      for (int i = 0; i < EPL; i += 4) *reinterpret_cast<u32x4*>(s_key + e0 + i) = u32x4{key[i], key[i + 1], key[i + 2], key[i + 3]};
+      __builtin_amdgcn_wave_barrier();
+      uint32_t value[4], left[4];
+      float low[4], size_of[4];    // the smallest c that counts in a group's value, and how large those are
+#pragma unroll
+      for (int gi = 0; gi < 4; ++gi) {
+        value[gi] = left[gi] = 0u;
+        low[gi] = size_of[gi] = 0.0f;
+        const int g = j16 + 16 * gi;
+        if (16 * gi < a.groups && g < a.groups) {
+          uint32_t k1 = 0u, k2 = 0u;
+          auto take = [&](uint32_t k) {
+            k2 = max(k2, min(k1, k));
+            k1 = max(k1, k);
+          };
+          int j = 0;
+          if ((size & 3) == 0) {
+#pragma unroll 4
+            for (; j < size; j += 4) {
+              const u32x4 k = *reinterpret_cast<const u32x4*>(s_key + g * size + j);
+              take(k.x); take(k.y); take(k.z); take(k.w);
+            }
+          }
+          for (; j < size; ++j) take(s_key[g * size + j]);
+          const float v1 = key_value(k1), v2 = key_value(k2);
+          value[gi] = left[gi] = a.best == 1 ? k1 : order_key(v1 + v2);
+          low[gi] = a.best == 1 ? v1 : v2;
+          size_of[gi] = fabsf(v1) + (a.best == 1 ? 0.0f : fabsf(v2));
+        }
+      }
+      __builtin_amdgcn_wave_barrier();
+      uint32_t last = 0u;
+      unsigned long long kept = 0ull;
+      for (int j = 0; j < a.top_groups; ++j) {
+        last = row_max(max(max(left[0], left[1]), max(left[2], left[3])));
+        uint32_t g = GROUPS_MAX;
+#pragma unroll
+        for (int gi = 3; gi >= 0; --gi)
+          if (left[gi] == last) g = j16 + 16 * gi;                           // (last is not 0: more groups than are kept)
+        g = row_min(g);
+        kept |= 1ull << g;
+#pragma unroll
+        for (int gi = 0; gi < 4; ++gi) left[gi] = j16 + 16 * gi == (int)g ? 0u : left[gi];
+      }
+      // the border between the last group kept and the best one left: who may be on either side of it
+      const float vk = key_value(last), vn = key_value(row_max(max(max(left[0], left[1]), max(left[2], left[3]))));
+      bool close = false;
+      float thr[4];
+#pragma unroll
+      for (int gi = 0; gi < 4; ++gi) {
+        const float v = key_value(value[gi]);
+        const float moved = 2.0f * a.best * off(0.5f * size_of[gi]) + 1e-6f * size_of[gi];      // two values, of one or two c each
+        const bool in = !whole && value[gi] != 0u && size_of[gi] < INFINITY && vk - vn <= moved && v >= vk - moved && v <= vn + moved;
+        thr[gi] = in ? low[gi] - moved : INFINITY;
+        close |= in;
+      }
+      if (__any(close)) {
+#pragma unroll
+        for (int gi = 0; gi < 4; ++gi) s_thr[j16 + 16 * gi] = thr[gi];
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) {
+          const float c = key_value(key[i]);
+          if (key[i] != 0u && ((exact >> i) & 1u) == 0u && fabsf(c) < INFINITY && c >= s_thr[(uint32_t)(e0 + i) * per_group >> 16]) again |= 1u << i;
+        }
+        __builtin_amdgcn_wave_barrier();
+      }
+      if (by_logit) alike = (vk != vn && vk - vn <= 2e-6f * fmaxf(1.0f, fabsf(vk))) || vk - m < -70.0f;
+      else if (!a.sigmoid) alike = close;
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) cur[i] = (kept >> ((uint32_t)(e0 + i) * per_group >> 16)) & 1ull ? cur[i] : 0u;
+    }
+    unsigned allowed = 0u;
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) allowed |= cur[i] != 0u ? 1u << i : 0u;
+
+    auto best_left = [&]() {
+      uint32_t k = cur[0];
+#pragma unroll
+      for (int i = 1; i < EPL; ++i) k = max(k, cur[i]);
+      return row_max(k);
+    };
+    float my_c = 0.0f, before = __uint_as_float(0x7fc00000u), s_before = 0.0f, most = 0.0f;
+    bool close = false;
+    auto compare = [&](float c, int e) {     // with the one chosen before it (a NaN or an infinite one is what it is)
+      const float d = before - c, large = fmaxf(fabsf(before), fabsf(c));
+      const bool both = large < INFINITY;
+      close |= both && d <= 2.0f * off(large);
+      most = both ? fmaxf(most, large) : most;
+      if (by_logit) {
+        alike |= both && d > 0.0f && d <= 4e-7f * fmaxf(1.0f, large);
+      } else if (!a.sigmoid) {               // between exact logits what is left is the denominator's error
+        const float sc = a.balance != nullptr ? c - s_bal[e] : c;
+        alike |= both && d <= 2.1f * doubt * fabsf(s_before - sc) + 5e-7f * (large + fabsf(sc));
+        s_before = sc;
+      }
+      before = c;
+    };
+    float next = __uint_as_float(0x7fc00000u);     // the border: the best one that is not chosen
+    for (int j = 0; j <= a.K; ++j) {         // (the last one is not chosen: the border)
+      const uint32_t k = best_left();
+      uint32_t e = 256u;
+#pragma unroll
+      for (int i = EPL - 1; i >= 0; --i)
+        if (cur[i] == k) e = (uint32_t)(e0 + i);
+      e = row_min(e);
+      const float c = key_value(k);
+      if (k != 0u) compare(c, (int)e);       // (no expert is left only behind the last choice)
+      if (j == a.K) {
+        next = c;
+        break;
+      }
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) cur[i] = e == (uint32_t)(e0 + i) ? 0u : cur[i];
+      if (by_logit) alike |= c - m < -70.0f;
+      if (j16 == j) { my_id = (int)e; my_c = c; }
+    }
+    close = close && !whole;
+    if (__any(close)) {      // whose logits lie that near to another's, at or above the border of the choice
+      const float width = 2.0f * off(most);
+      unsigned one = 0u, two = 0u;           // experts with a chosen value, or two, that near (a chosen one's own counts)
+      for (int j = 0; j <= a.K; ++j) {
+        const float c = j < a.K ? __shfl(my_c, (lane & 48) + j, WAVE) : next;
+        unsigned hit = 0u;
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) hit |= fabsf(key_value(key[i]) - c) <= width ? 1u << i : 0u;
+        two |= one & hit;
+        one |= j < a.K ? hit : 0u;           // (the border concerns the chosen alone)
+      }
+      unsigned chosen = 0u;
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) chosen |= cur[i] == 0u ? 1u << i : 0u;
+      if (close) again |= (chosen & two & allowed) | (~chosen & one & allowed);
+      again &= ~exact;
+    }
+    if (!whole && !redo) redo = !row_any(again != 0u) && row_any(alike);
+    if (redo || !want) again = 0u;
+    unsigned long long todo = __ballot(again != 0u);
+    if (todo == 0ull) break;
+    exact |= again;
+    unsigned bits = 0u;
+    int owner = 0;
+    while (todo != 0ull || bits != 0u) {     // two logits at a time
+      int at[2], slot[2];
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        if (bits == 0u && todo != 0ull) {
+          owner = __builtin_ctzll(todo);
+          todo &= todo - 1ull;
+          bits = (unsigned)__builtin_amdgcn_readlane((int)again, owner);
+        }
+        at[n] = owner;
+        slot[n] = bits != 0u ? __builtin_ctz(bits) : slot[0];                // (none left: the first one once more)
+        bits &= bits - 1u;
+      }
+      const bf16_t *xs[2], *ws[2];
+      float v[2];
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        xs[n] = a.x + (size_t)__builtin_amdgcn_readlane(t, at[n]) * a.H;
+        ws[n] = a.Wr + (size_t)(EPL * (at[n] & 15) + slot[n]) * a.H;
+      }
+      defined_logits(xs, ws, a.H, lane, v);
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        const int e = EPL * (at[n] & 15) + slot[n];
+        const float score = a.sigmoid ? (float)sigmoid64(v[n]) : by_logit ? v[n] : (float)(exp((double)v[n] - (double)m) / z);
+        const uint32_t k = order_key(a.balance != nullptr ? score + s_bal[e] : score);     // (of the owner's token: the owner's)
+        if (lane == at[n]) {
+          s_logit[e] = v[n];
+#pragma unroll
+          for (int q = 0; q < EPL; ++q) key[q] = q == slot[n] ? k : key[q];
+        }
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+  if (by_logit) {            // the weights' denominator
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) sum += e0 + i < a.E ? expf(s_logit[e0 + i] - m) : 0.0f;
+    z = row_sum(sum);
+  }
+  float s = 0.0f;
+  if (j16 < a.K) {
+    const float l = s_logit[my_id];
+    s = a.sigmoid ? 1.0f / (1.0f + expf(-l)) : expf(l - m) / (float)z;
+  }
+  if (a.renorm) s = s / (row_sum(s) + 1e-20f);
+  if (j16 < a.K && want && !redo) {
+    a.ids[(size_t)t * a.K + j16] = my_id;
+    a.w[(size_t)t * a.K + j16] = s * a.scale;
+  }
+  return redo;
+}
+
+// A workgroup of eight waves takes 16 * TT tokens and all experts (NBLK blocks of 16); each wave an eighth of K, so that every
+// byte of the router and of the rows is read once per workgroup, with no barrier on the way.  16 rows by 128 bytes are two
+// copies of 1 KB straight into the wave's own ring in LDS, whole lines with eight lanes side by side on a row, and come back
+// as operands from there.  (Loaded as operands, 16 rows by 16 bytes per 16 lanes, they took four times as long: 0.35 us per
+// block and wave, of the address unit.)  The eight partial sums meet in LDS, eight tiles at a time, and are added in the order
+// of the parts: a logit's bits depend on H alone.  The squares for the error bound are summed from the same operands.
+constexpr int ROUTE_WAVES = 8, ROUTE_RING = 8;                               // items of 2 KB in a wave's ring
+template <int NBLK, int TT>
+struct RouteShape {
+  static constexpr int TOKENS = 16 * TT, EP = 16 * NBLK, LDL = EP + 4;       // logits [TOKENS][LDL]
+  static constexpr int RINGS = ROUTE_WAVES * ROUTE_RING * 2048;              // then: parts (later keys and thresholds), logits behind them
+  static constexpr int PARTS = ROUTE_WAVES * 8 * 1024, LOGITS = TOKENS * LDL * 4, NORMS = ROUTE_WAVES * 4 * (1 + TOKENS) * 4, BAL = EP * 4;
+  static constexpr int LDS = RINGS + NORMS + BAL;
+  static_assert(RINGS >= PARTS + LOGITS && PARTS >= TOKENS * (EP + GROUPS_MAX) * 4 && LDS <= 160 * 1024, "LDS");
+};
+
+template <int NBLK, int TT>
+__global__ __launch_bounds__(64 * ROUTE_WAVES) void route_scored_kernel(RouteScored a) {
+  using S = RouteShape<NBLK, TT>;
+  extern __shared__ __align__(16) unsigned char smem[];
+  float* const s_logit = reinterpret_cast<float*>(smem + S::PARTS);
+  float* const s_wn = reinterpret_cast<float*>(smem + S::RINGS);             // [wave][g], then [TOKENS][wave][g]
+  float* const s_xn = s_wn + ROUTE_WAVES * 4;
+  float* const s_bal = s_xn + ROUTE_WAVES * 4 * S::TOKENS;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r16 = lane & 15, g = lane >> 4;
+  const int t0 = blockIdx.x * S::TOKENS;
+  const int H = a.H, nk = H / 64;
+  const int k0 = nk * wave / ROUTE_WAVES, k1 = nk * (wave + 1) / ROUTE_WAVES;
+
+  // A block's first expert: the last ones start early enough to have 16 rows (the overlap is formed twice, alike); with fewer
+  // than 16 experts, and for the last tokens, the last row is read again.
+  auto first = [&](int b) { return max(0, min(16 * b, a.E - 16)); };
+  const int crow = lane >> 3, cchunk = (lane & 7) ^ crow;                    // slot lane%8 of row lane/8 holds chunk slot xor row%8
+  uint32_t woff[2], xoff[TT][2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    woff[i] = (uint32_t)min(8 * i + crow, a.E - 1) * (uint32_t)H * 2u + 16u * cchunk;
+#pragma unroll
+    for (int tt = 0; tt < TT; ++tt) xoff[tt][i] = (uint32_t)min(16 * tt + 8 * i + crow, a.T - 1 - t0) * (uint32_t)H * 2u + 16u * cchunk;
+  }
+  unsigned char* const ring = smem + wave * ROUTE_RING * 2048;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)ring;
+  const bf16_t* const x0 = a.x + (size_t)t0 * H;
+  constexpr int NQ = TT + NBLK;                                              // items of a K step: token tiles, then experts
+  auto issue = [&](int j, int k, int slot) {                                 // item j of step k
+    const unsigned char* base = reinterpret_cast<const unsigned char*>((j < TT ? x0 : a.Wr + (size_t)first(j - TT) * H) + 64 * min(k, k1 - 1));
+#pragma unroll
+    for (int i = 0; i < 2; ++i) copy_to_lds_16(base, j < TT ? xoff[j < TT ? j : 0][i] : woff[i], lds0 + (uint32_t)slot * 2048u + (uint32_t)i * 1024u);
+  };
+  auto squares = [&](u32x4 v, float s) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const unsigned long long hit = __ballot(!out[i] && key[i] == k);
-      if (e < 0 && hit != 0ull) {
-        e = __builtin_ctzll(hit) + 64 * i;
-        mine = s[i];
+      const uint32_t pair = v[i];      // (a bit cast of the element itself takes the vector's first)
+      const bf16x2 p = __builtin_bit_cast(bf16x2, pair);
+      s = __builtin_amdgcn_fdot2_f32_bf16(p, p, s, false);
+    }
+    return s;
+  };
+  f32x4 acc[NBLK][TT];
+  float wn[NBLK], xn[TT];
+#pragma unroll
+  for (int b = 0; b < NBLK; ++b) {
+    wn[b] = 0.0f;
+#pragma unroll
+    for (int tt = 0; tt < TT; ++tt) acc[b][tt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+#pragma unroll
+  for (int tt = 0; tt < TT; ++tt) xn[tt] = 0.0f;
+  if (k0 < k1) {
+    constexpr int AHEAD = ROUTE_RING - 1;                                    // items in flight
+#pragma unroll
+    for (int q = 0; q < AHEAD; ++q) issue(q % NQ, k0 + q / NQ, q);
+    int slot = 0;
+    u32x4 xa[TT][2];
+    for (int k = k0; k < k1; ++k) {
+#pragma unroll
+      for (int j = 0; j < NQ; ++j) {
+        wait_copies_but<2 * (AHEAD - 1)>();
+        const unsigned char* st = ring + slot * 2048 + r16 * 128;
+        u32x4 v0 = *reinterpret_cast<const u32x4*>(st + ((g ^ (r16 & 7)) << 4));
+        u32x4 v1 = *reinterpret_cast<const u32x4*>(st + (((4 + g) ^ (r16 & 7)) << 4));
+        asm volatile("" : "+v"(v0), "+v"(v1));                               // in registers: the slot read before may be filled again
+        issue((j + AHEAD) % NQ, k + (j + AHEAD) / NQ, slot == 0 ? ROUTE_RING - 1 : slot - 1);
+        slot = slot + 1 == ROUTE_RING ? 0 : slot + 1;
+        if (j < TT) {
+          xa[j < TT ? j : 0][0] = v0;
+          xa[j < TT ? j : 0][1] = v1;
+          xn[j < TT ? j : 0] = squares(v1, squares(v0, xn[j < TT ? j : 0]));
+        } else {
+          const int b = j < TT ? 0 : j - TT;
+          wn[b] = squares(v1, squares(v0, wn[b]));
+#pragma unroll
+          for (int tt = 0; tt < TT; ++tt) {
+            acc[b][tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(v0), as_bf16x8(xa[tt][0]), acc[b][tt], 0, 0, 0);
+            acc[b][tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(v1), as_bf16x8(xa[tt][1]), acc[b][tt], 0, 0, 0);
+          }
+        }
       }
     }
-    const float sj = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mine), e & 63));
+  }
+  wait_copies_but<0>();
+  // squares: of each part of K the largest expert's (their sum is at least the largest sum), and every token's
+  float wpart = wn[0];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (e == lane + 64 * i) out[i] = true;
-    run += sj;
-    if (lane == j) { my_id = e; my_s = sj; }
-  }
-  if (a.renorm) my_s = my_s / (run + 1e-20f);
-  if (lane < a.K) {
-    a.ids[(size_t)t * a.K + lane] = my_id;
-    a.w[(size_t)t * a.K + lane] = my_s * a.scale;
-  }
-}
-
-// The logit of one (token, expert) pair by one wave, in the defined order
-__device__ __forceinline__ float defined_logit(const bf16_t* x, const bf16_t* w, int H, int lane) {
-  float acc = 0.0f;
-  for (int h = 8 * lane; h < H; h += 512) {
-    float xf[8], wf[8];
-    widen8(*reinterpret_cast<const u32x4*>(x + h), xf);
-    widen8(*reinterpret_cast<const u32x4*>(w + h), wf);
+  for (int b = 1; b < NBLK; ++b) wpart = fmaxf(wpart, wn[b]);
+  wpart = row_max(wpart);
+  if (r16 == 0) s_wn[wave * 4 + g] = wpart;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) acc = __builtin_fmaf(xf[i], wf[i], acc);
-  }
-  return fold_sum(acc);
-}
-
-__global__ __launch_bounds__(256) void route_scored_kernel(RouteScored a) {
-  __shared__ float s_logit[SCORED_EMAX];
-  __shared__ uint32_t s_key[SCORED_EMAX];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, t = blockIdx.x;
-  for (int e = wave; e < a.E; e += 4) {
-    const float l = defined_logit(a.x + (size_t)t * a.H, a.Wr + (size_t)e * a.H, a.H, lane);
-    if (lane == 0) s_logit[e] = l;
+  for (int tt = 0; tt < TT; ++tt) s_xn[(16 * tt + r16) * (ROUTE_WAVES * 4) + wave * 4 + g] = xn[tt];
+  for (int e = tid; e < S::EP; e += 64 * ROUTE_WAVES) s_bal[e] = a.balance != nullptr && e < a.E ? a.balance[e] : 0.0f;
+  // tile v = b * TT + tt of a round of eight is summed by wave v % 8; the parts take the place of the rings
+  f32x4* const s_part = reinterpret_cast<f32x4*>(smem);                      // [wave][8][lane]
+#pragma unroll
+  for (int r = 0; r < NBLK * TT; r += 8) {
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < 8; ++v)
+      if (r + v < NBLK * TT) s_part[(wave * 8 + v) * 64 + lane] = acc[(r + v) / TT][(r + v) % TT];
+    __syncthreads();
+    const int v = r + wave;
+    if (v < NBLK * TT) {
+      f32x4 sum = s_part[wave * 64 + lane];
+#pragma unroll
+      for (int w = 1; w < ROUTE_WAVES; ++w) sum += s_part[(w * 8 + wave) * 64 + lane];
+      // element j: expert first + 4 g + j of token r16
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s_logit[(16 * (v % TT) + r16) * S::LDL + first(v / TT) + 4 * g + j] = sum[j];
+    }
   }
   __syncthreads();
-  if (wave != 0) return;
-  float l[4], s[4];
-  uint32_t key[4];
+  float bal_most = 0.0f;
+  if (a.balance != nullptr && !a.sigmoid) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) l[i] = lane + 64 * i < a.E ? s_logit[lane + 64 * i] : 0.0f;
-  form_scores(a, l, lane, s);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int e = lane + 64 * i;
-    key[i] = order_key(a.balance != nullptr && e < a.E ? s[i] + a.balance[e] : s[i]);
+    for (int e = lane; e < S::EP; e += 64) bal_most = fmaxf(bal_most, fabsf(s_bal[e]) < INFINITY ? fabsf(s_bal[e]) : 0.0f);
+    bal_most = fold_max(bal_most);
   }
-  choose(a, key, s, lane, s_key, t);
+  const int tk = (wave * 4 + (lane >> 4)) % S::TOKENS, t = t0 + tk;          // (waves without tokens of their own help out only)
+  const float w2 = row_sum(s_wn[r16] + s_wn[16 + r16]), x2 = row_sum(s_xn[tk * 32 + r16] + s_xn[tk * 32 + 16 + r16]);
+  const bool known = x2 >= 1e-30f && x2 < INFINITY && w2 >= 1e-30f && w2 < INFINITY;     // (squares that did not vanish or overflow)
+  uint32_t* const s_key = reinterpret_cast<uint32_t*>(smem) + tk * (S::EP + GROUPS_MAX);
+  const float doubt = known ? LOGIT_ERROR * fmaxf(1.0f, (float)H / 2048.0f) * sqrtf(x2) * sqrtf(w2) : -1.0f;
+  int* const s_redo = reinterpret_cast<int*>(s_wn);                          // (every wave has read the norms before the barrier below)
+  bool redo = false;
+  for (int pass = 0; pass < 2; ++pass) {
+    if (wave * 4 < S::TOKENS)
+      redo = choose<NBLK>(a, min(t, a.T - 1), t < a.T && (pass == 0 || redo), pass > 0 && redo, s_logit + tk * S::LDL, s_bal, bal_most, doubt,
+                          lane, s_key, reinterpret_cast<float*>(s_key + S::EP)) && t < a.T;
+    if (pass > 0 || !__syncthreads_or(redo)) break;
+    // the tokens that need all of their logits in the defined order (values that are not finite, softmax scores too close to
+    // tell apart by a denominator that is not exact): by all waves
+    if (r16 == 0 && wave * 4 < S::TOKENS) s_redo[tk] = redo;
+    __syncthreads();
+    for (int i = 0; i < S::TOKENS; ++i) {
+      if (s_redo[i] == 0) continue;
+      for (int e = 4 * wave; e < a.E; e += 4 * ROUTE_WAVES) {
+        const bf16_t *xs[1] = {x0 + (size_t)i * H}, *ws[4];
+        float v[4];
+#pragma unroll
+        for (int n = 0; n < 4; ++n) ws[n] = a.Wr + (size_t)min(e + n, a.E - 1) * H;
+        defined_logits(xs, ws, H, lane, v);
+        if (lane == 0) *reinterpret_cast<f32x4*>(s_logit + i * S::LDL + e) = f32x4{v[0], v[1], v[2], v[3]};
+      }
+    }
+    __syncthreads();
+  }
 }
 
-int launch_route_scored(const RouteScored& a, hipStream_t st) {
-  hipLaunchKernelGGL(route_scored_kernel, dim3(a.T), dim3(256), 0, st, a);
+template <int NBLK, int TT>
+int launch_route_scored_t(const RouteScored& a, hipStream_t st) {
+  using S = RouteShape<NBLK, TT>;
+  auto kern = route_scored_kernel<NBLK, TT>;
+  static std::atomic<uint64_t> lds_raised{0};
+  if (raise_lds_limit((const void*)kern, S::LDS, lds_raised) != 0) return -4;
+  hipLaunchKernelGGL(kern, dim3((a.T + S::TOKENS - 1) / S::TOKENS), dim3(64 * ROUTE_WAVES), S::LDS, st, a);
   return hipGetLastError() == hipSuccess ? 0 : -4;
+}
+
+}  // namespace
+
+int launch_route_scored(const RouteScored& a, hipStream_t st) {
+  const bool many = a.T > 16 * 256;      // more than a workgroup of 16 tokens per compute unit
+  if (a.E <= 64) return many ? launch_route_scored_t<4, 2>(a, st) : launch_route_scored_t<4, 1>(a, st);
+  if (a.E <= 128) return many ? launch_route_scored_t<8, 2>(a, st) : launch_route_scored_t<8, 1>(a, st);
+  if (a.E <= 192) return many ? launch_route_scored_t<12, 2>(a, st) : launch_route_scored_t<12, 1>(a, st);
+  return many ? launch_route_scored_t<16, 2>(a, st) : launch_route_scored_t<16, 1>(a, st);
 }
 
 }  // namespace moe

@@ -145,7 +145,7 @@ def m0_hazards_in_kernel(body: List[str]) -> List[Tuple[str, str]]:
 
 # kernels in which every LDS access of a wave must have finished before the wave issues its next copy into LDS (the tile
 # kernels copy into one stage while they read another, behind barriers)
-_WAVE_PRIVATE_RING = "expert_stream"
+_WAVE_PRIVATE_RING = ("expert_stream", "route_scored")
 
 
 def ring_hazards_in_kernel(body: List[str]) -> List[Tuple[str, str]]:
@@ -188,7 +188,7 @@ def check_file(path: str) -> List[str]:
         m0 = m0_hazards_in_kernel(body)
         if m0:
             out.append(f"{name}: {len(m0)} LDS-writing load(s) directly behind the write of m0, e.g. `{m0[0][0]}` / `{m0[0][1]}`")
-        ring = ring_hazards_in_kernel(body) if _WAVE_PRIVATE_RING in name else []
+        ring = ring_hazards_in_kernel(body) if any(n in name for n in _WAVE_PRIVATE_RING) else []
         if ring:
             out.append(f"{name}: {len(ring)} pair(s) of an LDS access and a copy into LDS issued before it has finished, "
                        f"e.g. `{ring[0][0]}` / `{ring[0][1]}`")

@@ -3,8 +3,9 @@
 Tolerances.  Conversion of bf16 rows: to the bit (the scale follows from bits, the quotient is exact, one rounding).  Norm: a
 sum of squares of up to 8192 values is at most 42 fp32 roundings long (32 per lane, 8 joins, 2), half of that after the root,
 and six more steps: 2^-19 of the value covers it; bf16 rounds by 2^-8 at most, e4m3 by 2^-4 of the value or, below its normal
-range, half of 2^-9 * scale.  Gating: ids equal; weights 64-bit sigmoid or softmax rounded to fp32, a sum of at most 16, a
-quotient and a product: 2^-20.  Expert rows: element by element what mx_reference.experts bounds; and, much closer, the 2-norm
+range, half of 2^-9 * scale.  Gating: ids equal; weights: logits are fp32 sums in some order, off by at most 32 * 2^-24
+(beyond H 2048 H / 64 * 2^-24) of |x[t]| * max |Wr[e]| (a step of 32 products by 6 * 2^-24 of its terms' magnitudes), which moves a softmax or sigmoid by at most
+twice that of its value and a renormalised one by twice that again; sum, quotient and product 2^-20.  Expert rows: element by element what mx_reference.experts bounds; and, much closer, the 2-norm
 over a row: two roundings to bf16 (of the hidden row, of the output), each uniform within 2^-8 at most, are 2^-8 / sqrt(3) in
 the mean square or less, together 3.2e-3; the matrix instruction's own cuts 1e-4.  A row's 64 to 16384 elements scatter around
 that: twice it is allowed for a row, and it for a batch of 2048 elements and more."""
@@ -156,7 +157,8 @@ def check_route(moe, x, Wr, b, K, score, G, top, best, renorm, scale):
     finite = torch.isfinite(rw)
     w = w.cpu().double()
     assert torch.equal(torch.isnan(w), torch.isnan(rw))
-    assert bool(((w - rw).abs() <= 2.0 ** -20 * rw.abs() + 1e-38)[finite].all())
+    doubt = max(32, x.shape[1] / 64) * 2.0 ** -24 * x.double().norm(dim=1, keepdim=True) * Wr.double().norm(dim=1).max()
+    assert bool(((w - rw).abs() <= (4 * doubt + 2.0 ** -20) * rw.abs() + 1e-38)[finite].all())
     return ids, w
 
 
