@@ -419,43 +419,56 @@ def moe_residual_norm(x, y, out=None, eps: float = 1e-6):
     return out
 
 
-def _here(what: str, **tensors) -> None:
-    """All given tensors on the current device, whose stream the call takes."""
-    for name, t in tensors.items():
-        if t is not None and (not t.is_cuda or t.device.index != torch.cuda.current_device()):
-            raise MoeError(f"{what}: {name} must be on the current GPU, it is on {t.device}")
+# The calls on 8-bit rows are short (a decode step's take 2 to 4 us on the GPU), so their checks are one pass per tensor: a call
+# of one token costs the host 5 to 8 us, with a helper per check 11 to 21.
+_E4M3, _E8M0, _BF16, _F32, _I32 = torch.float8_e4m3fn, torch.float8_e8m0fnu, torch.bfloat16, torch.float32, torch.int32
 
 
-def _mx(pair, shape, name: str, what: str):
-    """Addresses of an 8-bit tensor's values (of the given shape) and scales."""
-    q, scales = pair
-    if tuple(q.shape) != tuple(shape) or tuple(scales.shape) != (*shape[:-1], shape[-1] // 32):
-        raise MoeError(f"{what}: {name} must be values {tuple(shape)} with scales {(*shape[:-1], shape[-1] // 32)}, "
-                       f"got {tuple(q.shape)} and {tuple(scales.shape)}")
-    _here(what, **{name: q, f"{name} scales": scales})
-    return _ptr(q, torch.float8_e4m3fn, name), _ptr(scales, torch.float8_e8m0fnu, f"{name} scales")
-
-
-def _as(t, shape, name: str, what: str):
-    if t is not None and tuple(t.shape) != tuple(shape):
+def _at(t, dtype, shape, name: str, what: str, dev: int) -> Optional[int]:
+    """Address of a tensor that is contiguous, on GPU `dev` (the current one, whose stream the call takes), and of this dtype (None:
+    any) and shape; None for None."""
+    if t is None:
+        return None
+    if (dtype is None or t.dtype is dtype) and t.is_contiguous() and t.get_device() == dev and (shape is None or t.shape == shape):
+        return t.data_ptr()
+    if shape is not None and tuple(t.shape) != tuple(shape):
         raise MoeError(f"{what}: {name} must be {tuple(shape)}, got {tuple(t.shape)}")
-    return t
+    if dtype is not None and t.dtype is not dtype:
+        raise MoeError(f"{what}: {name} must be {dtype}, got {t.dtype}")
+    if not t.is_contiguous():
+        raise MoeError(f"{what}: {name} must be contiguous")
+    raise MoeError(f"{what}: {name} must be on the current GPU, it is on {t.device}")
+
+
+def _scales_shape(shape):
+    return (*shape[:-1], shape[-1] // 32)
+
+
+def _device(t, name: str, what: str) -> int:
+    """The current GPU, where `t` must be (its stream is the call's)."""
+    dev = t.get_device()
+    if dev < 0 or dev != torch._C._cuda_getDevice():
+        raise MoeError(f"{what}: {name} must be on the current GPU, it is on {t.device}")
+    return dev
 
 
 def moe_quantize_mx(x, q=None, scales=None):
     """bf16 x [.., H] as 8-bit values: (q [.., H] float8_e4m3fn, scales [.., H / 32] float8_e8m0fnu), one scale per 32
     neighbours of the last dimension."""
-    H = x.shape[-1]
+    what, shape = "moe_quantize_mx", x.shape
+    H = shape[-1]
     if H % 64 != 0 or H == 0:
-        raise MoeError(f"moe_quantize_mx: the last dimension must be a multiple of 64, got {H}")
-    _here("moe_quantize_mx", x=x)
+        raise MoeError(f"{what}: the last dimension must be a multiple of 64, got {H}")
+    dev = _device(x, "x", what)
+    x_p = _at(x, _BF16, shape, "x", what, dev)
     if q is None:
-        q = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=x.device)
+        q = torch.empty_like(x, dtype=_E4M3)
     if scales is None:
-        scales = torch.empty((*x.shape[:-1], H // 32), dtype=torch.float8_e8m0fnu, device=x.device)
-    q_p, s_p = _mx((q, scales), x.shape, "q", "moe_quantize_mx")
-    rc = load().moe_quantize_mx(_ptr(x, torch.bfloat16, "x"), x.numel() // H, H, q_p, s_p, _stream())
-    _check(rc, "moe_quantize_mx")
+        scales = torch.empty(_scales_shape(shape), dtype=_E8M0, device=x.device)
+    rc = load().moe_quantize_mx(x_p, x.numel() // H, H, _at(q, _E4M3, shape, "q", what, dev),
+                                _at(scales, _E8M0, _scales_shape(shape), "scales", what, dev), torch._C._cuda_getCurrentRawStream(dev))
+    if rc != 0:
+        _check(rc, what)
     return q, scales
 
 
@@ -463,25 +476,25 @@ def moe_residual_norm_mx(x, y=None, weight=None, eps: float = 1e-6, sum=None, ou
                          keep_sum: bool = True, keep_out: bool = True, quantize: bool = True):
     """u = x + y (y None: x); n = u / sqrt(mean(u^2) + eps) * weight.  Returns (sum = bf16(u), out = bf16(n), q, scales = n in
     8 bits), None for what is not wanted.  sum and out may be x or y."""
-    what = "moe_residual_norm_mx"
-    T, H = x.shape
+    what, shape = "moe_residual_norm_mx", x.shape
+    T, H = shape
     if H % 64 != 0:
         raise MoeError(f"{what}: H must be a multiple of 64, got {H}")
-    _as(y, (T, H), "y", what), _as(weight, (H,), "weight", what)
-    _here(what, x=x, y=y, weight=weight, sum=sum, out=out)
-    sum = (torch.empty_like(x) if sum is None else _as(sum, (T, H), "sum", what)) if keep_sum else None
-    out = (torch.empty_like(x) if out is None else _as(out, (T, H), "out", what)) if keep_out else None
-    q_p = s_p = None
+    dev = _device(x, "x", what)
+    y_p, w_p = _at(y, _BF16, shape, "y", what, dev), _at(weight, _BF16, (H,), "weight", what, dev)
+    x_p = _at(x, _BF16, shape, "x", what, dev)
+    sum = (torch.empty_like(x) if sum is None else sum) if keep_sum else None
+    out = (torch.empty_like(x) if out is None else out) if keep_out else None
     if quantize:
-        q = torch.empty((T, H), dtype=torch.float8_e4m3fn, device=x.device) if q is None else q
-        scales = torch.empty((T, H // 32), dtype=torch.float8_e8m0fnu, device=x.device) if scales is None else scales
-        q_p, s_p = _mx((q, scales), (T, H), "q", what)
+        q = torch.empty_like(x, dtype=_E4M3) if q is None else q
+        scales = torch.empty((T, H // 32), dtype=_E8M0, device=x.device) if scales is None else scales
     else:
         q = scales = None
-    bf = torch.bfloat16
-    rc = load().moe_residual_norm_mx(_ptr(x, bf, "x"), _ptr(y, bf, "y"), _ptr(weight, bf, "weight"), T, H, float(eps),
-                                     _ptr(sum, bf, "sum"), _ptr(out, bf, "out"), q_p, s_p, _stream())
-    _check(rc, what)
+    rc = load().moe_residual_norm_mx(x_p, y_p, w_p, T, H, eps, _at(sum, _BF16, shape, "sum", what, dev), _at(out, _BF16, shape, "out", what, dev),
+                                     _at(q, _E4M3, shape, "q", what, dev), _at(scales, _E8M0, (T, H // 32), "scales", what, dev),
+                                     torch._C._cuda_getCurrentRawStream(dev))
+    if rc != 0:
+        _check(rc, what)
     return sum, out, q, scales
 
 
@@ -498,18 +511,18 @@ def moe_route_scored(x, Wr, balance, K: int, score: str = "softmax", groups: int
         raise MoeError(f"{what}: score must be one of {sorted(SCORES)}, got {score!r}")
     T, H = x.shape
     E = Wr.shape[0]
-    _as(Wr, (E, H), "Wr", what), _as(balance, (E,), "balance", what)
-    _as(topk_ids, (T, K), "topk_ids", what), _as(topk_w, (T, K), "topk_w", what)
-    _here(what, x=x, Wr=Wr, balance=balance, topk_ids=topk_ids, topk_w=topk_w)
+    dev = _device(x, "x", what)
+    Wr_p, b_p = _at(Wr, _BF16, (E, H), "Wr", what, dev), _at(balance, _F32, (E,), "balance", what, dev)
+    x_p = _at(x, _BF16, None, "x", what, dev)
     if topk_ids is None:
-        topk_ids = torch.empty((T, K), dtype=torch.int32, device=x.device)
+        topk_ids = torch.empty((T, K), dtype=_I32, device=x.device)
     if topk_w is None:
-        topk_w = torch.empty((T, K), dtype=torch.float32, device=x.device)
-    rc = load().moe_route_scored(_ptr(x, torch.bfloat16, "x"), _ptr(Wr, torch.bfloat16, "Wr"), _ptr(balance, torch.float32, "balance"),
-                                 T, H, E, int(K), SCORES[score], int(groups), int(top_groups), int(group_best), int(bool(renorm)),
-                                 float(scale), _ptr(topk_ids, torch.int32, "topk_ids"), _ptr(topk_w, torch.float32, "topk_w"),
-                                 _stream())
-    _check(rc, what)
+        topk_w = torch.empty((T, K), dtype=_F32, device=x.device)
+    rc = load().moe_route_scored(x_p, Wr_p, b_p, T, H, E, K, SCORES[score], groups, top_groups, group_best, 1 if renorm else 0, scale,
+                                 _at(topk_ids, _I32, (T, K), "topk_ids", what, dev), _at(topk_w, _F32, (T, K), "topk_w", what, dev),
+                                 torch._C._cuda_getCurrentRawStream(dev))
+    if rc != 0:
+        _check(rc, what)
     return topk_ids, topk_w
 
 
@@ -519,21 +532,26 @@ def moe_expert_group_forward_mx(group_lo: int, group_hi: int, x, src_of_row, K: 
     what = "moe_expert_group_forward_mx"
     E, I, H = Wg[0].shape
     P = Yp.shape[0]
-    if src_of_row is not None and (K < 1 or src_of_row.numel() != P or x[0].shape[0] * K != P):
+    if src_of_row is not None and (K < 1 or src_of_row.shape != (P,) or x[0].shape[0] * K != P):
         raise MoeError(f"{what}: x must have P / K rows and src_of_row P entries")
     if expert_offsets.numel() != E + 1:
         raise MoeError(f"{what}: expert_offsets must have E + 1 entries")
-    _as(Yp, (P, H), "Yp", what)
-    x_p = _mx(x, (P if src_of_row is None else P // K, H), "x", what)
-    w_p = [a for name, w, n, k in (("Wg", Wg, I, H), ("Wu", Wu, I, H), ("Wd", Wd, H, I)) for a in _mx(w, (E, n, k), name, what)]
+    dev = _device(Yp, "Yp", what)
+    rows, up, down = (P if src_of_row is None else P // K, H), (E, I, H), (E, H, I)
+    up_s, down_s = (E, I, H // 32), (E, H, I // 32)
     if workspace is None:
-        workspace = torch.empty(max(int(load().moe_expert_workspace_bytes(P, I)), 256), dtype=torch.uint8, device=Yp.device)
-    _here(what, src_of_row=src_of_row, expert_offsets=expert_offsets, Yp=Yp, workspace=workspace)
-    rc = load().moe_expert_group_forward_mx(int(group_lo), int(group_hi), *x_p, _ptr(src_of_row, torch.int32, "src_of_row"), int(K),
-                                            _ptr(expert_offsets, torch.int32, "expert_offsets"), *w_p, P, H, E, I,
-                                            _ptr(Yp, torch.bfloat16, "Yp"), _ptr(workspace, None, "workspace"),
-                                            workspace.numel() * workspace.element_size(), _stream())
-    _check(rc, what)
+        workspace = torch.empty(max(P * I * 2, 256), dtype=torch.uint8, device=Yp.device)
+    rc = load().moe_expert_group_forward_mx(
+        group_lo, group_hi, _at(x[0], _E4M3, rows, "x", what, dev), _at(x[1], _E8M0, (rows[0], H // 32), "x scales", what, dev),
+        _at(src_of_row, _I32, None, "src_of_row", what, dev), K,
+        _at(expert_offsets, _I32, None, "expert_offsets", what, dev),
+        _at(Wg[0], _E4M3, up, "Wg", what, dev), _at(Wg[1], _E8M0, up_s, "Wg scales", what, dev),
+        _at(Wu[0], _E4M3, up, "Wu", what, dev), _at(Wu[1], _E8M0, up_s, "Wu scales", what, dev),
+        _at(Wd[0], _E4M3, down, "Wd", what, dev), _at(Wd[1], _E8M0, down_s, "Wd scales", what, dev), P, H, E, I,
+        _at(Yp, _BF16, (P, H), "Yp", what, dev), _at(workspace, None, None, "workspace", what, dev), workspace.nbytes,
+        torch._C._cuda_getCurrentRawStream(dev))
+    if rc != 0:
+        _check(rc, what)
     return Yp
 
 

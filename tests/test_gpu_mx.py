@@ -332,6 +332,37 @@ def test_scales_far_apart_and_zero_rows(moe):
     assert not bool(Yp[7].float().any())
 
 
+def test_binding_refuses_tensors_of_another_shape_type_layout_or_device(moe):
+    x = rows(4, 128, 1).cuda()
+    bad = lambda match, call: _refused(moe, match, call)
+    q, s = moe.moe_quantize_mx(x)
+    bad("x must be contiguous", lambda: moe.moe_quantize_mx(torch.zeros((64, 64), dtype=torch.bfloat16, device="cuda").t()))
+    bad("x must be torch.bfloat16", lambda: moe.moe_quantize_mx(x.float()))
+    bad("q must be", lambda: moe.moe_quantize_mx(x, q=q[:2]))
+    bad("scales must be", lambda: moe.moe_quantize_mx(x, scales=s.view(torch.uint8)))
+    bad("y must be", lambda: moe.moe_residual_norm_mx(x, x[:2]))
+    bad("weight must be", lambda: moe.moe_residual_norm_mx(x, None, x[0, :64]))
+    bad("weight must be on the current GPU", lambda: moe.moe_residual_norm_mx(x, None, x[0].cpu()))
+    bad("sum must be", lambda: moe.moe_residual_norm_mx(x, sum=x[:, :64].contiguous()))
+    bad("Wr must be", lambda: moe.moe_route_scored(x, x[:, :64].contiguous(), None, 2))
+    bad("balance must be", lambda: moe.moe_route_scored(x, x, torch.zeros(5).cuda(), 2))
+    bad("topk_ids must be", lambda: moe.moe_route_scored(x, x, None, 2, topk_ids=torch.zeros(4, 2).cuda()))
+    c = block_case(moe, [2, 2], 128, 64, 1)
+    run = lambda **kw: run_block(moe, dict(c, **kw))
+    bad("x must be", lambda: run(x=moe.moe_quantize_mx(x[:3].contiguous())))
+    bad("x scales must be", lambda: run(x=(c["x"][0], c["x"][1][:, :2].contiguous())))
+    bad("Wu must be", lambda: run(Wu=c["Wd"]))
+    bad("Wd scales must be", lambda: run(Wd=(c["Wd"][0], c["Wu"][1])))
+    bad("Yp must be", lambda: run_block(moe, c, Yp=torch.zeros((4, 64), dtype=torch.bfloat16, device="cuda")))
+    bad("workspace too small", lambda: moe.moe_expert_group_forward_mx(0, 2, c["x"], None, 1, c["off"], c["Wg"], c["Wu"], c["Wd"], run_block(moe, c),
+                                                                       torch.zeros(16, dtype=torch.uint8, device="cuda")))
+
+
+def _refused(moe, match, call):
+    with pytest.raises(moe.MoeError, match=match):
+        call()
+
+
 # ---- together, as a serving loop uses them
 
 def layer(moe, s):

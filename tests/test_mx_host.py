@@ -71,38 +71,26 @@ def test_expert_block_refusals(lib):
     assert call(x=None, P=0) == 0
 
 
-def test_binding_refuses_what_the_library_cannot_see():
+def test_binding_refuses_before_it_looks_at_a_gpu():
     import paper_2604_26881_amd as moe
     x = torch.zeros(4, 64, dtype=torch.bfloat16)
-    with pytest.raises(moe.MoeError, match="on the current GPU"):
-        moe.moe_quantize_mx(x)
     with pytest.raises(moe.MoeError, match="multiple of 64"):
         moe.moe_quantize_mx(x[:, :32])
-    with pytest.raises(moe.MoeError, match="weight must be"):
-        moe.moe_residual_norm_mx(x, None, torch.zeros(32))
-    with pytest.raises(moe.MoeError, match="y must be"):
-        moe.moe_residual_norm_mx(x, x[:2])
+    with pytest.raises(moe.MoeError, match="multiple of 64"):
+        moe.moe_residual_norm_mx(x[:, :32])
     with pytest.raises(moe.MoeError, match="score must be"):
         moe.moe_route_scored(x, x, None, 2, score="relu")
-    with pytest.raises(moe.MoeError, match="balance must be"):
-        moe.moe_route_scored(x, x, torch.zeros(5), 2)
-    with pytest.raises(moe.MoeError, match="Wr must be"):
-        moe.moe_route_scored(x, x[:, :32], None, 2)
-    e4, e8 = torch.float8_e4m3fn, torch.float8_e8m0fnu
-    pair = lambda *s: (torch.zeros(s, dtype=torch.uint8).view(e4), torch.zeros((*s[:-1], s[-1] // 32), dtype=torch.uint8).view(e8))
-    W, Wd, off, Y = pair(2, 64, 64), pair(2, 64, 64), torch.zeros(3, dtype=torch.int32), torch.zeros(4, 64, dtype=torch.bfloat16)
-    src = torch.zeros(4, dtype=torch.int32)
-    call = lambda x=pair(4, 64), src=None, K=1, off=off, Wg=W, Y=Y: moe.moe_expert_group_forward_mx(0, 2, x, src, K, off, Wg, W, Wd, Y)
+    pair = lambda *s: (torch.zeros(s, dtype=torch.uint8).view(torch.float8_e4m3fn),
+                       torch.zeros((*s[:-1], s[-1] // 32), dtype=torch.uint8).view(torch.float8_e8m0fnu))
+    W, off, Y, src = pair(2, 64, 64), torch.zeros(3, dtype=torch.int32), torch.zeros(4, 64, dtype=torch.bfloat16), torch.zeros(4, dtype=torch.int32)
+    block = lambda src=None, K=1, off=off: moe.moe_expert_group_forward_mx(0, 2, pair(4, 64), src, K, off, W, W, W, Y)
     with pytest.raises(moe.MoeError, match="P / K rows"):
-        call(src=src, K=2)
+        block(src=src, K=2)
     with pytest.raises(moe.MoeError, match="E . 1 entries"):
-        call(off=off[:2])
-    with pytest.raises(moe.MoeError, match="x must be values"):
-        call(x=pair(3, 64))
-    with pytest.raises(moe.MoeError, match="x must be values"):
-        call(x=(pair(4, 64)[0], pair(4, 32)[1]))
-    with pytest.raises(moe.MoeError, match="on the current GPU"):
-        call()
+        block(off=off[:2])
+    for call in (lambda: moe.moe_quantize_mx(x), lambda: moe.moe_residual_norm_mx(x), lambda: moe.moe_route_scored(x, x, None, 2), block):
+        with pytest.raises(moe.MoeError, match="on the current GPU"):
+            call()
 
 
 def test_reference_conversion_is_torchs_where_nothing_saturates():
