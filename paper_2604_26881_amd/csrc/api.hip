@@ -715,10 +715,9 @@ int moe_expert_group_forward_mx(int group_lo, int group_hi, const void* x, const
   gu.gather = src_of_row; gu.gather_div = src_of_row ? K : 1;
   dn.A = (const uint8_t*)workspace; dn.As = nullptr; dn.B0 = (const uint8_t*)Wd; dn.B0s = (const uint8_t*)Wd_scales; dn.B1 = dn.B1s = nullptr;
   dn.C = (bf16_t*)Yp; dn.N = H; dn.Kdim = I;
-  const bool tiles = gu.mean_rows > 32;
-  const int rc = tiles ? launch_tile_mx_gateup(gu, (hipStream_t)stream) : launch_stream_mx_gateup(gu, (hipStream_t)stream);
+  const int rc = mx_in_tiles(gu) ? launch_tile_mx_gateup(gu, (hipStream_t)stream) : launch_stream_mx_gateup(gu, (hipStream_t)stream);
   if (rc != 0) return rc;
-  return tiles ? launch_tile_mx_down(dn, (hipStream_t)stream) : launch_stream_mx_down(dn, (hipStream_t)stream);
+  return mx_in_tiles(dn) ? launch_tile_mx_down(dn, (hipStream_t)stream) : launch_stream_mx_down(dn, (hipStream_t)stream);
 }
 
 }  // extern "C"

@@ -10,9 +10,10 @@
 // tiles, experts with few and with many tiles are drawn in turn).
 //
 // K steps of 128 (gate/up) or 64 (down: a bf16 row has as many bytes) through a ring of NS LDS stages filled by asynchronous
-// copies, a row's 16-byte chunks xor-swizzled against bank conflicts; one barrier per step.  The scales of a step come with
-// it, one 4-byte slot per row: gate/up four scale bytes (a contraction that is not whole steps has rows of scales on odd
-// multiples of two bytes: then two slots of two bytes), down two.
+// copies, a row's 16-byte chunks xor-swizzled against bank conflicts; one barrier per step.  Scales come 16 bytes of a row at a
+// time, those of 4 (gate/up) or 8 steps, into a ring of their own: every row is another cache line, and fetched step by step
+// they cost as many line requests as the rows themselves (one expert of 16 384 rows, H 8192, I 4096, gate/up: 1004 us, this way 916,
+// without any scales 872).
 //
 // Gate/up multiplies with 32x32x64 on 8-bit values: a lane holds of row lane % 32 the chunks 4m + h and 4m + 2 + h of the
 // step's half m (h = lane / 32) and gives the scale of block 2m + h: the row's slot, shifted by h bytes, and a byte select.
@@ -34,7 +35,7 @@ namespace {
 
 constexpr int TILE_MX_EMAX = 256;
 
-template <int BM, bool GATEUP, int NS, bool PAIR>
+template <int BM, bool GATEUP, int NS, bool TAIL>
 struct TileMxShape {
   static constexpr int BN = 256, WAVES_M = 2, WAVES_N = 4, NW = 8;
   static constexpr int TB = BM / 64, NB = 2;                // 32-row blocks of a wave: tokens, weights
@@ -43,29 +44,34 @@ struct TileMxShape {
   static constexpr int WROWB = GATEUP ? 128 : 64;           // bytes per staged weight row (token rows: 128)
   static constexpr int SROWS = GATEUP ? BM + BN : BN;       // rows with scales
   static constexpr int TOKENS = BM * 128, WEIGHTS = BN * WROWB;
-  static constexpr int STAGE = TOKENS + WEIGHTS + SROWS * 4 * (PAIR ? 2 : 1);
+  static constexpr int STAGE = TOKENS + WEIGHTS;
+  static constexpr int SB = GATEUP ? 4 : 2, GS = 16 / SB;   // scale bytes per row and step, steps per group of 16 bytes
+  static constexpr int RING = NS == 2 || (GATEUP && BM == 128) ? 2 : 3;     // groups in LDS
+  static constexpr int SCALES = SROWS * 16, LDS = NS * STAGE + RING * SCALES + 16;    // (a last row's pair of dwords ends behind it)
   static constexpr int NLA = BM / 64;                       // 1 KB copies per wave and stage: token rows,
-  static constexpr int NLB = GATEUP ? 4 : 2;                // weight rows,
-  static constexpr int NLS = PAIR ? 2 : 1;                  // scales (64 rows each)
-  static constexpr int NL = NLA + NLB + NLS;
+  static constexpr int NLB = GATEUP ? 4 : 2;                // weight rows (and, once per group, scales of 64 rows)
+  static constexpr int NL = NLA + NLB;
   static constexpr int GM = 4;                              // token tiles per locality group of the walk
-  static_assert(GATEUP || !PAIR, "the down projection's steps have two scale bytes");
-  static_assert(NS >= 2 && NS * NL < 64 && NS * STAGE <= 160 * 1024, "wait counter and LDS");
+  static_assert(GATEUP || !TAIL, "the down projection's steps are half as long");
+  static_assert(NS >= 2 && NS * NL < 60 && LDS <= 160 * 1024 && SROWS / 64 <= NW, "wait counter, LDS, a copy of scales per wave");
 };
+constexpr int TILE_MX_MIN_K = 512;       // a row has 16 scale bytes
 
-// One value of SZ bytes per lane into LDS, four bytes apart (zero-extended)
-template <int SZ>
-__device__ __forceinline__ void copy_to_lds_small(const void* base, uint32_t voff, uint32_t lds) {
-  if constexpr (SZ == 2)
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_ushort %0, %1" ::"v"(voff), "s"(base), "s"(lds) : "memory", "m0");
-  else
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(voff), "s"(base), "s"(lds) : "memory", "m0");
+template <int N>
+using number = std::integral_constant<int, N>;
+template <int FROM, int TO, class F>
+__device__ __forceinline__ void for_range(F&& f) {
+  if constexpr (FROM < TO) {
+    f(number<FROM>{});
+    for_range<FROM + 1, TO>(f);
+  }
 }
 
-template <int BM, bool GATEUP, int NS, bool PAIR, bool SINGLE>
+template <int BM, bool GATEUP, int NS, bool TAIL, bool SINGLE>
 __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
-  using S = TileMxShape<BM, GATEUP, NS, PAIR>;
+  using S = TileMxShape<BM, GATEUP, NS, TAIL>;
   extern __shared__ __align__(16) unsigned char smem[];
+  constexpr bool EARLY = BM < 256;
   constexpr int HEAVY_MIN = 3;       // token tiles from which an expert counts as bound by the matrix cores
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -116,6 +122,7 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
   const int crow = lane >> 3, cchunk = (lane & 7) ^ crow;   // copies of 128-byte rows: row lane/8, slot lane%8 holding chunk slot xor row%8
   const int r32 = lane & 31, half = lane >> 5, swz = lane & 7;
+  const int sgrp = wave % (S::SROWS / 64);                  // 64 rows of scales (waves past the last group have none)
   const uint32_t tail_back = GATEUP && cchunk >= 4 ? 64u : 0u;
 
   const int G = gridDim.x;
@@ -124,34 +131,48 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
   const int run = xcd_walk ? max(1, min(G >> 3, (Lend + 7) >> 3)) : 1;
   if (xcd_walk && slot >= run) return;
 
-  struct Tile { int row0, rowEnd, tbv, n0; bool once, valid; };
+  struct Tile { int row0, rowEnd, first_row, eg, rows, tbv, n0; bool once, valid; };
   const uint8_t *Ag = nullptr, *Bg0 = nullptr, *Bg1 = nullptr, *Sg = nullptr;
   uint32_t coff[S::NLA + S::NLB], soff = 0;     // byte offsets of this lane's parts of a stage's copies, at K step 0
   int krot = 0;
   auto kstep = [&](int kt) -> int { const int k = kt + krot; return k >= nk ? k - nk : k; };
-  auto issue = [&](int kt, int st, auto once_) {
-    const int k = kstep(min(kt, nk - 1));       // (past the end the last step again: the wait counts stay constant)
-    const uint32_t l = lds0 + (uint32_t)st * S::STAGE + (uint32_t)wave * 1024u;
-    const uint32_t back = PAIR && k == nk - 1 ? tail_back : 0u;     // the missing half from the half that is there
-#pragma unroll
-    for (int i = 0; i < S::NLA; ++i) copy_to_lds_16(Ag + (size_t)k * 128, coff[i] - back, l + (uint32_t)i * 8192u);
-#pragma unroll
-    for (int i = 0; i < S::NLB; ++i)
-      copy_to_lds_16((GATEUP && i >= 2 ? Bg1 : Bg0) + (size_t)k * S::WROWB, coff[S::NLA + i] - back, l + (uint32_t)(S::TOKENS + i * 8192),
-                     decltype(once_)::value);
-    const uint32_t ls = lds0 + (uint32_t)st * S::STAGE + (uint32_t)(S::TOKENS + S::WEIGHTS) + (uint32_t)(wave % (S::SROWS / 64)) * 256u;
-    if constexpr (!GATEUP) {
-      copy_to_lds_small<2>(Sg + 2 * (size_t)k, soff, ls);
-    } else if constexpr (PAIR) {
-      copy_to_lds_small<2>(Sg + 4 * (size_t)k, soff, ls);
-      copy_to_lds_small<2>(Sg + 4 * (size_t)k + (k == nk - 1 ? 0 : 2), soff, ls + (uint32_t)S::SROWS * 4u);
+  // copy i of a stage: token rows, weight rows, scales
+  auto issue1 = [&](int k, int st, auto i_, auto once_) {
+    constexpr int i = decltype(i_)::value;
+    const uint32_t l = lds0 + (uint32_t)st * S::STAGE;
+    const uint32_t back = TAIL && k == nk - 1 ? tail_back : 0u;     // the missing half from the half that is there
+    if constexpr (i < S::NLA) {
+      copy_to_lds_16(Ag + (size_t)k * 128, coff[i] - back, l + (uint32_t)wave * 1024u + (uint32_t)i * 8192u);
     } else {
-      copy_to_lds_small<4>(Sg + 4 * (size_t)k, soff, ls);
+      copy_to_lds_16((GATEUP && i >= S::NLA + 2 ? Bg1 : Bg0) + (size_t)k * S::WROWB, coff[i] - back,
+                     l + (uint32_t)wave * 1024u + (uint32_t)(S::TOKENS + (i - S::NLA) * 8192), decltype(once_)::value);
+    }
+  };
+  // copies [FROM, TO) of K step kt (past the end the last step again: the wait counts stay constant) into stage buffer st
+  auto issue = [&](int kt, int st, auto from_, auto to_, auto once_) {
+    const int k = kstep(min(kt, nk - 1));
+    for_range<decltype(from_)::value, decltype(to_)::value>([&](auto i_) { issue1(k, st, i_, once_); });
+  };
+  // Scales: 16 bytes of a row are GS steps.  The last group of a row that is not whole groups starts earlier instead, so that it
+  // ends with the row.
+  auto group_start = [&](int k) { return min(k / S::GS * 16, kb32 - 16); };
+  int group_in = 0, group_out = 0;       // ring slots of the next group to be requested and of the one that is read
+  // before the copies of K step kt the scales, if a group begins there.  (The copy is not counted in the waits, which makes them
+  // wait for one copy more than they must.)
+  auto issue_scales = [&](int kt) {
+    const int k = kstep(min(kt, nk - 1));
+    if (k % S::GS == 0 && kt < nk) {
+      if (wave < S::SROWS / 64)
+        copy_to_lds_16(Sg + group_start(k), soff, lds0 + (uint32_t)(NS * S::STAGE + group_in * S::SCALES) + (uint32_t)wave * 1024u);
+      group_in = group_in + 1 == S::RING ? 0 : group_in + 1;
     }
   };
 
   int it = 0;
-  auto next_tile = [&]() -> Tile {
+  // The next tile of this workgroup and, in gathered[], the token rows that this lane copies of it (requested while the current
+  // tile is multiplied: its first copies then wait for nothing).
+  int gathered[S::NLA + 1];
+  auto find_tile = [&]() -> Tile {
     Tile t{};
     int mrow = 0, nt = 0, cls = 0;
     for (;; ++it) {
@@ -180,26 +201,34 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
       ve = mine ? re[i] : ve;
     }
     const int owner = __builtin_ctzll(found);
-    const int eg = a.lo + owner * 4 + __builtin_amdgcn_readlane(at, owner);
-    const int rb_e = __builtin_amdgcn_readlane(vb, owner);
-    t.row0 = rb_e + (mrow - __builtin_amdgcn_readlane(vf, owner)) * BM;
+    t.eg = a.lo + owner * 4 + __builtin_amdgcn_readlane(at, owner);
+    t.first_row = __builtin_amdgcn_readlane(vb, owner);
+    t.row0 = t.first_row + (mrow - __builtin_amdgcn_readlane(vf, owner)) * BM;
     t.rowEnd = __builtin_amdgcn_readlane(ve, owner);
-    const int rows = min(BM, t.rowEnd - t.row0);
-    t.tbv = min(S::TB, max(1, (((rows + 31) >> 5) - wm + S::WAVES_M - 1) / S::WAVES_M));
+    t.rows = min(BM, t.rowEnd - t.row0);
+    t.tbv = min(S::TB, max(1, (((t.rows + 31) >> 5) - wm + S::WAVES_M - 1) / S::WAVES_M));
     t.n0 = nt * S::NOUT;
-    t.once = SINGLE && t.rowEnd - rb_e <= BM;
-    auto token = [&](int r) -> int {
-      const int row = t.row0 + min(r, rows - 1);
-      return GATEUP && a.gather != nullptr ? a.gather[row] / a.gather_div : row;
-    };
+    t.once = SINGLE && t.rowEnd - t.first_row <= BM;
+    if (GATEUP && a.gather != nullptr) {
+#pragma unroll
+      for (int i = 0; i < S::NLA; ++i) gathered[i] = a.gather[t.row0 + min((i * S::NW + wave) * 8 + crow, t.rows - 1)];
+      gathered[S::NLA] = a.gather[t.row0 + min(sgrp * 64 + lane, t.rows - 1)];
+    }
+    return t;
+  };
+  auto request_tile = [&](const Tile& t) {
+    if (!t.valid) return;
+    // row r of the tile, the i-th this lane copies
+    auto token = [&](int r, int i) -> int { return GATEUP && a.gather != nullptr ? gathered[i] / a.gather_div : t.row0 + min(r, t.rows - 1); };
     auto column = [&](int r) { return min(t.n0 + r, N - 1); };
+    const int eg = t.eg;
     Ag = a.A;
     const size_t wrow = (size_t)eg * N;
     Bg0 = a.B0 + wrow * Kdim;
     Bg1 = GATEUP ? a.B1 + wrow * Kdim : nullptr;
 #pragma unroll
     for (int i = 0; i < S::NLA; ++i)
-      coff[i] = (uint32_t)token((i * S::NW + wave) * 8 + crow) * (uint32_t)(GATEUP ? Kdim : 2 * Kdim) + (uint32_t)cchunk * 16u;
+      coff[i] = (uint32_t)token((i * S::NW + wave) * 8 + crow, i) * (uint32_t)(GATEUP ? Kdim : 2 * Kdim) + (uint32_t)cchunk * 16u;
 #pragma unroll
     for (int i = 0; i < S::NLB; ++i) {
       if (GATEUP)        // copies of 8 rows; the second half of the rows: the up branch
@@ -207,25 +236,29 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
       else               // of 16 rows: row lane/4, slot lane%4 holding chunk slot xor (row/4)%4
         coff[S::NLA + i] = (uint32_t)column((i * S::NW + wave) * 16 + (lane >> 2)) * (uint32_t)Kdim + (uint32_t)((lane & 3) ^ ((lane >> 4) & 3)) * 16u;
     }
-    const int sgrp = wave % (S::SROWS / 64);     // 64 rows of scales (waves past the last group copy one a second time)
     if (GATEUP && sgrp < BM / 64) {
       Sg = a.As;
-      soff = (uint32_t)token(sgrp * 64 + lane) * (uint32_t)kb32;
+      soff = (uint32_t)token(sgrp * 64 + lane, S::NLA) * (uint32_t)kb32;
     } else {
       const int w = sgrp - (GATEUP ? BM / 64 : 0);
       Sg = (GATEUP && w >= 2 ? a.B1s : a.B0s) + wrow * kb32;
       soff = (uint32_t)column((GATEUP ? w & 1 : w) * 64 + lane) * (uint32_t)kb32;
     }
-    krot = SINGLE && t.once ? (int)((unsigned)(eg * 5 + t.n0 / S::NOUT * 3) % (unsigned)nk) : 0;
-#pragma unroll
-    for (int s = 0; s < NS - 1; ++s) {
-      if (SINGLE && t.once) issue(s, s, std::true_type{}); else issue(s, s, std::false_type{});
+    // (whole groups of scales; with two groups in LDS none may be shorter than the others)
+    const unsigned groups = (unsigned)(nk + S::GS - 1) / S::GS;
+    krot = SINGLE && t.once && (S::RING > 2 || nk % S::GS == 0) ? (int)((unsigned)(eg * 5 + t.n0 / S::NOUT * 3) % groups) * S::GS : 0;
+    for (int s = 0; s < NS; ++s) {
+      issue_scales(s);
+      if (SINGLE && t.once) issue(s, s, number<0>{}, number<S::NL>{}, std::true_type{});
+      else issue(s, s, number<0>{}, number<S::NL>{}, std::false_type{});
     }
-    return t;
   };
 
-  Tile cur = next_tile();
+  Tile cur = find_tile();
+  request_tile(cur);
   while (cur.valid) {
+    Tile nxt;
+    if constexpr (EARLY) nxt = find_tile();
     f32x16 acc[S::NB][S::TB];
 #pragma unroll
     for (int nb = 0; nb < S::NB; ++nb)
@@ -234,75 +267,166 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[nb][tb][i] = 0.0f;
 
+    // Software pipeline.  All NS stages of the tile have been requested (next_tile).  A step is cut into slots of matrix
+    // instructions; a slot's operands are read from LDS during the slot before, those of a step's first slot during the last slot of
+    // the step before, behind the barrier that publishes the step's stage.  That barrier also says that everybody has the step
+    // before it in registers, so its buffer takes the copies of the stage NS steps ahead: a part in that slot, the rest in the
+    // first two slots of the next step (at the first step they repeat copies of the prologue: the same bytes to the same place).
     auto pipeline = [&](auto tbc_, auto once_) {
       constexpr int TBc = decltype(tbc_)::value;
-      auto scale_of = [&](const unsigned char* sc, int row) -> uint32_t {
-        const uint32_t lo = *reinterpret_cast<const uint32_t*>(sc + row * 4);
-        return PAIR ? lo | *reinterpret_cast<const uint32_t*>(sc + (S::SROWS + row) * 4) << 16 : lo;
-      };
+      constexpr int SLOTS = GATEUP ? 2 * TBc : 4;
+      constexpr int PART0 = S::NL - 2 * (S::NL / 3), PART1 = SLOTS > 2 ? PART0 + S::NL / 3 : S::NL;
       auto wrow = [&](int nb) { return (GATEUP ? nb * 128 + wn * 32 : wn * 64 + nb * 32) + r32; };
       auto trow = [&](int tb) { return (tb * S::WAVES_M + wm) * 32 + r32; };
+      auto slot_copies = [&](auto s_, int kt, int st) {
+        constexpr int s = decltype(s_)::value;
+        const int before = st == 0 ? NS - 1 : st - 1;
+        if constexpr (s == SLOTS - 1) issue(kt + NS, st, number<0>{}, number<PART0>{}, once_);
+        if constexpr (s == 0) issue(kt - 1 + NS, before, number<PART0>{}, number<PART1>{}, once_);
+        if constexpr (s == 1 && SLOTS > 2) issue(kt - 1 + NS, before, number<PART1>{}, number<S::NL>{}, once_);
+      };
+      auto publish = [&]() {                      // before a step's last slot
+        wait_lds_reads();
+        wait_copies_but<(NS - 2) * S::NL>();      // the next stage has landed
+        workgroup_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+      };
+      // at the top of a step: the scales of the stage requested next, and where those of the next step (byte `scale_at` of each
+      // row's 16, in LDS at `scales`) will be
+      const unsigned char* scales = smem + NS * S::STAGE + group_out * S::SCALES;
+      int scale_at = S::SB * krot - group_start(krot);
+      auto scales_top = [&](int kt) {
+        issue_scales(kt + NS);
+        const int k = kstep(min(kt + 1, nk - 1));
+        if (kt + 1 < nk && k % S::GS == 0) group_out = group_out + 1 == S::RING ? 0 : group_out + 1;
+        scales = smem + NS * S::STAGE + group_out * S::SCALES;
+        scale_at = S::SB * k - group_start(k);
+      };
+      wait_copies_but<(NS - 1) * S::NL>();
+      workgroup_barrier();
       int st = 0;
-      for (int kt = 0; kt < nk; ++kt) {
-        wait_lds_reads();                         // (of stage kt - 1)
-        wait_copies_but<(NS - 2) * S::NL>();      // stage kt has landed
-        workgroup_barrier();                      // for everyone; and everyone has read stage kt - 1, whose buffer is free
-        issue(kt + NS - 1, st == 0 ? NS - 1 : st - 1, once_);
-        const unsigned char* base = smem + st * S::STAGE;
-        const unsigned char* sc = base + S::TOKENS + S::WEIGHTS;
-        if constexpr (GATEUP) {
-          int sw[S::NB], sx[TBc];
+      if constexpr (GATEUP) {
+        u32x4 w[2][S::NB][2], x[2][2];            // weights of the step's two halves; token blocks of this slot and the next
+        uint32_t sw[S::NB], sx[TBc];              // scale slots, shifted to the lane's block
+        auto read_row = [&](u32x4 (&v)[2], const unsigned char* row, auto m_) {
+          constexpr int m = decltype(m_)::value;
+          v[0] = *reinterpret_cast<const u32x4*>(row + (((4 * m + half) ^ swz) << 4));
+          v[1] = *reinterpret_cast<const u32x4*>(row + (((4 * m + 2 + half) ^ swz) << 4));
+        };
+        auto read_w = [&](const unsigned char* base, auto m_) {
 #pragma unroll
-          for (int nb = 0; nb < S::NB; ++nb) sw[nb] = (int)(scale_of(sc, BM + wrow(nb)) >> (8 * half));
-#pragma unroll
-          for (int tb = 0; tb < TBc; ++tb) sx[tb] = (int)(scale_of(sc, trow(tb)) >> (8 * half));
-          const bool whole = !PAIR || kstep(kt) != nk - 1;
-          auto half_step = [&](auto m_) {
-            constexpr int m = decltype(m_)::value;
-            auto chunks = [&](const unsigned char* row) {
-              return mx_operand(*reinterpret_cast<const u32x4*>(row + (((4 * m + half) ^ swz) << 4)),
-                                *reinterpret_cast<const u32x4*>(row + (((4 * m + 2 + half) ^ swz) << 4)));
-            };
-            i32x8 w[S::NB];
-#pragma unroll
-            for (int nb = 0; nb < S::NB; ++nb) w[nb] = chunks(base + S::TOKENS + wrow(nb) * 128);
-#pragma unroll
-            for (int tb = 0; tb < TBc; ++tb) {
-              const i32x8 x = chunks(base + trow(tb) * 128);
-#pragma unroll
-              for (int nb = 0; nb < S::NB; ++nb)
-                acc[nb][tb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w[nb], x, acc[nb][tb], 0, 0, 2 * m, sw[nb], 2 * m, sx[tb]);
-            }
+          for (int nb = 0; nb < S::NB; ++nb) read_row(w[decltype(m_)::value][nb], base + S::TOKENS + wrow(nb) * 128, m_);
+        };
+        auto read_x = [&](const unsigned char* base, auto s_) {
+          constexpr int s = decltype(s_)::value;
+          read_row(x[s & 1], base + trow(s % TBc) * 128, number<s / TBc>{});
+        };
+        auto read_scales = [&]() {
+          const unsigned char* sc = scales + (scale_at & ~3);
+          auto one = [&](int row) -> uint32_t {
+            const uint32_t lo = *reinterpret_cast<const uint32_t*>(sc + row * 16);
+            if constexpr (!TAIL) return lo >> (8 * half);
+            // (in the last group of a row of an odd number of pairs the step's bytes begin at an odd pair)
+            return __builtin_amdgcn_alignbit(*reinterpret_cast<const uint32_t*>(sc + row * 16 + 4), lo, (scale_at & 2) * 8) >> (8 * half);
           };
-          half_step(std::integral_constant<int, 0>{});
-          if (whole) half_step(std::integral_constant<int, 1>{});
-        } else {
-          uint32_t sw[S::NB];
 #pragma unroll
-          for (int nb = 0; nb < S::NB; ++nb) sw[nb] = scale_of(sc, wrow(nb));
+          for (int nb = 0; nb < S::NB; ++nb) sw[nb] = one(BM + wrow(nb));
 #pragma unroll
-          for (int p = 0; p < 2; ++p) {
-            u32x4 w[S::NB];
+          for (int tb = 0; tb < TBc; ++tb) sx[tb] = one(trow(tb));
+        };
+        read_scales();
+        read_w(smem, number<0>{});
+        read_x(smem, number<0>{});
+        for (int kt = 0; kt < nk; ++kt) {
+          const unsigned char* base = smem + st * S::STAGE;
+          const int st1 = st + 1 == NS ? 0 : st + 1;
+          scales_top(kt);
+          const bool whole = !TAIL || kstep(kt) != nk - 1;
+          for_range<0, SLOTS>([&](auto s_) {
+            constexpr int s = decltype(s_)::value, m = s / TBc, tb = s % TBc;
+            uint32_t sw0[S::NB], sx0 = sx[tb];
 #pragma unroll
-            for (int nb = 0; nb < S::NB; ++nb)
-              w[nb] = *reinterpret_cast<const u32x4*>(base + S::TOKENS + wrow(nb) * 64 + (((2 * p + half) ^ ((lane >> 2) & 3)) << 4));
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              bf16x8 wf[S::NB];
-#pragma unroll
-              for (int nb = 0; nb < S::NB; ++nb) wf[nb] = mx_to_bf16(w[nb][2 * j], w[nb][2 * j + 1], (int)((sw[nb] >> (8 * p)) & 255u));
-#pragma unroll
-              for (int tb = 0; tb < TBc; ++tb) {
-                const bf16x8 x = as_bf16x8(*reinterpret_cast<const u32x4*>(base + trow(tb) * 128 + (((4 * p + 2 * half + j) ^ swz) << 4)));
-#pragma unroll
-                for (int nb = 0; nb < S::NB; ++nb)
-                  acc[nb][tb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wf[nb], x, acc[nb][tb], 0, 0, 0);
-              }
+            for (int nb = 0; nb < S::NB; ++nb) sw0[nb] = sw[nb];
+            if constexpr (s == SLOTS - 1) publish();
+            auto multiply = [&](int nb) {
+              acc[nb][tb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(mx_operand(w[m][nb][0], w[m][nb][1]), mx_operand(x[s & 1][0], x[s & 1][1]),
+                                                                            acc[nb][tb], 0, 0, 2 * m, (int)sw0[nb], 2 * m, (int)sx0);
+            };
+            if (m == 0 || whole) multiply(0);
+            __builtin_amdgcn_sched_barrier(0x6);
+            if constexpr (s < SLOTS - 1) {
+              read_x(base, number<s + 1>{});
+              if constexpr (s == (TBc > 1 ? TBc - 2 : 0)) read_w(base, number<1>{});
+            } else {
+              const unsigned char* next = smem + st1 * S::STAGE;
+              read_x(next, number<0>{});
+              read_w(next, number<0>{});
+              read_scales();
             }
-          }
+            slot_copies(s_, kt, st);
+            __builtin_amdgcn_sched_barrier(0x6);
+            if (m == 0 || whole) multiply(1);
+            __builtin_amdgcn_sched_barrier(0x6);
+          });
+          st = st1;
         }
-        st = st + 1 == NS ? 0 : st + 1;
+      } else {
+        u32x4 raw[2][S::NB];                      // weights as they are, of the step's two halves
+        bf16x8 wf[2][S::NB], x[2][TBc];           // operands of this slot and the next
+        uint32_t sw[S::NB];
+        auto read_raw = [&](const unsigned char* base, auto p_) {
+          constexpr int p = decltype(p_)::value;
+#pragma unroll
+          for (int nb = 0; nb < S::NB; ++nb)
+            raw[p][nb] = *reinterpret_cast<const u32x4*>(base + S::TOKENS + wrow(nb) * 64 + (((2 * p + half) ^ ((lane >> 2) & 3)) << 4));
+        };
+        auto read_scales = [&]() {
+#pragma unroll
+          for (int nb = 0; nb < S::NB; ++nb) sw[nb] = *reinterpret_cast<const uint16_t*>(scales + scale_at + wrow(nb) * 16);
+        };
+        auto read_x1 = [&](const unsigned char* base, auto s_, int tb) {
+          constexpr int s = decltype(s_)::value;
+          x[s & 1][tb] = as_bf16x8(*reinterpret_cast<const u32x4*>(base + trow(tb) * 128 + (((4 * (s >> 1) + 2 * half + (s & 1)) ^ swz) << 4)));
+        };
+        auto convert = [&](auto s_) {
+          constexpr int s = decltype(s_)::value, p = s >> 1, j = s & 1;
+#pragma unroll
+          for (int nb = 0; nb < S::NB; ++nb) wf[j][nb] = mx_to_bf16(raw[p][nb][2 * j], raw[p][nb][2 * j + 1], (int)((sw[nb] >> (8 * p)) & 255u));
+        };
+        read_scales();
+        read_raw(smem, number<0>{});
+#pragma unroll
+        for (int tb = 0; tb < TBc; ++tb) read_x1(smem, number<0>{}, tb);
+        convert(number<0>{});
+        for (int kt = 0; kt < nk; ++kt) {
+          const unsigned char* base = smem + st * S::STAGE;
+          const int st1 = st + 1 == NS ? 0 : st + 1;
+          scales_top(kt);
+          for_range<0, SLOTS>([&](auto s_) {
+            constexpr int s = decltype(s_)::value;
+            if constexpr (s == SLOTS - 1) publish();
+            const unsigned char* from = s < SLOTS - 1 ? base : smem + st1 * S::STAGE;
+            constexpr int NM = S::NB * TBc;       // matrix instructions of the slot: behind the first ones the reads, then the copies
+#pragma unroll
+            for (int j = 0; j < NM; ++j) {
+              acc[j % S::NB][j / S::NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wf[s & 1][j % S::NB], x[s & 1][j / S::NB], acc[j % S::NB][j / S::NB], 0, 0, 0);
+              if (j == 0) {
+                if constexpr (s == 0) read_raw(base, number<1>{});
+                if constexpr (s == SLOTS - 1) {
+                  read_raw(from, number<0>{});
+                  read_scales();
+                }
+              }
+              if (j < TBc) read_x1(from, number<(s + 1) % SLOTS>{}, j);
+              if (j == (TBc < NM - 1 ? TBc : NM - 1)) slot_copies(s_, kt, st);
+              __builtin_amdgcn_sched_barrier(0x6);
+            }
+            convert(number<(s + 1) % SLOTS>{});
+          });
+          st = st1;
+        }
       }
+      group_out = group_out + 1 == S::RING ? 0 : group_out + 1;      // (the next tile begins a group)
       wait_lds_reads();
       wait_copies_but<0>();      // the repeated copies of the last steps: none may outlive the tile
       workgroup_barrier();       // the next tile's first copies overwrite stages that other waves may still read
@@ -317,7 +441,8 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
     };
     if (SINGLE && cur.once) run_pipeline(std::true_type{}); else run_pipeline(std::false_type{});
 
-    const Tile nxt = next_tile();      // its first copies fly while this tile is stored
+    if constexpr (!EARLY) nxt = find_tile();
+    request_tile(nxt);      // its first copies fly while this tile is stored
 
     // accumulator element i of block (nb, tb): column 8 (i / 4) + 4 half + i % 4 of the block, token row lane % 32; lanes l and
     // l + 32 trade four columns each, so that each stores 16 bytes
@@ -359,11 +484,12 @@ int num_cus() {
   return n;
 }
 
-template <int BM, bool GATEUP, int NS, bool PAIR, bool SINGLE>
+template <int BM, bool GATEUP, int NS, bool TAIL, bool SINGLE>
 int launch_tile_mx_t(const MxArgs& a, hipStream_t st) {
-  using S = TileMxShape<BM, GATEUP, NS, PAIR>;
-  auto kern = expert_tile_mx_kernel<BM, GATEUP, NS, PAIR, SINGLE>;
-  constexpr int lds = NS * S::STAGE;
+  using S = TileMxShape<BM, GATEUP, NS, TAIL>;
+  auto kern = expert_tile_mx_kernel<BM, GATEUP, NS, TAIL, SINGLE>;
+  constexpr int lds = S::LDS;
+  if (a.Kdim < TILE_MX_MIN_K) return -2;
   static std::atomic<uint64_t> lds_raised{0};
   const int nexp = a.hi - a.lo;
   if (nexp > TILE_MX_EMAX) return -2;

@@ -64,6 +64,8 @@ struct MxArgs {
 };
 int launch_stream_mx_gateup(const MxArgs& a, hipStream_t st);
 int launch_stream_mx_down(const MxArgs& a, hipStream_t st);
+// Tiles: more than 32 rows per expert, and a contraction long enough for their scales to come 16 bytes of a row at a time.
+inline bool mx_in_tiles(const MxArgs& a) { return a.mean_rows > 32 && a.Kdim >= 512; }
 int launch_tile_mx_gateup(const MxArgs& a, hipStream_t st);
 int launch_tile_mx_down(const MxArgs& a, hipStream_t st);
 
