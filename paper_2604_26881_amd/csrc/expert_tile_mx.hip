@@ -11,7 +11,7 @@
 //
 // K steps of 128 (gate/up) or 64 (down: a bf16 row has as many bytes) through a ring of NS LDS stages filled by asynchronous
 // copies, a row's 16-byte chunks xor-swizzled against bank conflicts; one barrier per step.  Scales come 16 bytes of a row at a
-// time, those of 4 (gate/up) or 8 steps, into a ring of their own: every row is another cache line, and fetched step by step
+// time, those of 4 (gate/up) or 8 steps, into two buffers of their own: every row is another cache line, and fetched step by step
 // they cost as many line requests as the rows themselves (one expert of 16 384 rows, H 8192, I 4096, gate/up: 1004 us, this way 916,
 // without any scales 872).
 //
@@ -22,9 +22,8 @@
 // run beside the other wave's matrix instructions.
 //
 // Rows past the end of an expert repeat its last row and are not stored; 32-row blocks of nothing but such rows are not
-// multiplied.  Experts whose rows fit one tile read every weight once: their tiles ask for weights with the read-once hint and
-// start their walk over K at a step of their own.  A row's bits depend on the tile height (picked from layer-wide sizes) and
-// that start (from expert and column), never on the block cut.
+// multiplied.  Weights are copied without a read-once hint: down reads a 128-byte line in two steps, and a hinted line was fetched
+// twice (60 experts of 64 rows, H 2048, I 1408: 66 us with it, 55 without).  A row's bits do not depend on the tile height.
 #include <math.h>
 #include <algorithm>
 #include <type_traits>
@@ -46,14 +45,14 @@ struct TileMxShape {
   static constexpr int TOKENS = BM * 128, WEIGHTS = BN * WROWB;
   static constexpr int STAGE = TOKENS + WEIGHTS;
   static constexpr int SB = GATEUP ? 4 : 2, GS = 16 / SB;   // scale bytes per row and step, steps per group of 16 bytes
-  static constexpr int RING = NS == 2 || (GATEUP && BM == 128) ? 2 : 3;     // groups in LDS
-  static constexpr int SCALES = SROWS * 16, LDS = NS * STAGE + RING * SCALES + 16;    // (a last row's pair of dwords ends behind it)
+  static constexpr int SCALES = SROWS * 16, LDS = NS * STAGE + 2 * SCALES + 16;    // (a last row's pair of dwords ends behind it)
   static constexpr int NLA = BM / 64;                       // 1 KB copies per wave and stage: token rows,
   static constexpr int NLB = GATEUP ? 4 : 2;                // weight rows (and, once per group, scales of 64 rows)
   static constexpr int NL = NLA + NLB;
   static constexpr int GM = 4;                              // token tiles per locality group of the walk
   static_assert(GATEUP || !TAIL, "the down projection's steps are half as long");
-  static_assert(NS >= 2 && NS * NL < 60 && LDS <= 160 * 1024 && SROWS / 64 <= NW, "wait counter, LDS, a copy of scales per wave");
+  static_assert(NS >= 2 && NS * NL < 60 && NS <= GS && LDS <= 160 * 1024 && SROWS / 64 <= NW,
+                "wait counter; two groups of scales in LDS are enough; LDS; a copy of scales per wave");
 };
 constexpr int TILE_MX_MIN_K = 512;       // a row has 16 scale bytes
 
@@ -67,7 +66,7 @@ __device__ __forceinline__ void for_range(F&& f) {
   }
 }
 
-template <int BM, bool GATEUP, int NS, bool TAIL, bool SINGLE>
+template <int BM, bool GATEUP, int NS, bool TAIL>
 __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
   using S = TileMxShape<BM, GATEUP, NS, TAIL>;
   extern __shared__ __align__(16) unsigned char smem[];
@@ -131,13 +130,11 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
   const int run = xcd_walk ? max(1, min(G >> 3, (Lend + 7) >> 3)) : 1;
   if (xcd_walk && slot >= run) return;
 
-  struct Tile { int row0, rowEnd, first_row, eg, rows, tbv, n0; bool once, valid; };
+  struct Tile { int row0, rowEnd, eg, rows, tbv, n0; bool valid; };
   const uint8_t *Ag = nullptr, *Bg0 = nullptr, *Bg1 = nullptr, *Sg = nullptr;
   uint32_t coff[S::NLA + S::NLB], soff = 0;     // byte offsets of this lane's parts of a stage's copies, at K step 0
-  int krot = 0;
-  auto kstep = [&](int kt) -> int { const int k = kt + krot; return k >= nk ? k - nk : k; };
   // copy i of a stage: token rows, weight rows, scales
-  auto issue1 = [&](int k, int st, auto i_, auto once_) {
+  auto issue1 = [&](int k, int st, auto i_) {
     constexpr int i = decltype(i_)::value;
     const uint32_t l = lds0 + (uint32_t)st * S::STAGE;
     const uint32_t back = TAIL && k == nk - 1 ? tail_back : 0u;     // the missing half from the half that is there
@@ -145,26 +142,26 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
       copy_to_lds_16(Ag + (size_t)k * 128, coff[i] - back, l + (uint32_t)wave * 1024u + (uint32_t)i * 8192u);
     } else {
       copy_to_lds_16((GATEUP && i >= S::NLA + 2 ? Bg1 : Bg0) + (size_t)k * S::WROWB, coff[i] - back,
-                     l + (uint32_t)wave * 1024u + (uint32_t)(S::TOKENS + (i - S::NLA) * 8192), decltype(once_)::value);
+                     l + (uint32_t)wave * 1024u + (uint32_t)(S::TOKENS + (i - S::NLA) * 8192));
     }
   };
   // copies [FROM, TO) of K step kt (past the end the last step again: the wait counts stay constant) into stage buffer st
-  auto issue = [&](int kt, int st, auto from_, auto to_, auto once_) {
-    const int k = kstep(min(kt, nk - 1));
-    for_range<decltype(from_)::value, decltype(to_)::value>([&](auto i_) { issue1(k, st, i_, once_); });
+  auto issue = [&](int kt, int st, auto from_, auto to_) {
+    const int k = min(kt, nk - 1);
+    for_range<decltype(from_)::value, decltype(to_)::value>([&](auto i_) { issue1(k, st, i_); });
   };
   // Scales: 16 bytes of a row are GS steps.  The last group of a row that is not whole groups starts earlier instead, so that it
   // ends with the row.
   auto group_start = [&](int k) { return min(k / S::GS * 16, kb32 - 16); };
-  int group_in = 0, group_out = 0;       // ring slots of the next group to be requested and of the one that is read
+  int group_in = 0, group_out = 0;       // the next group to be requested goes to the first, the one that is read lies in the second of these buffers
   // before the copies of K step kt the scales, if a group begins there.  (The copy is not counted in the waits, which makes them
   // wait for one copy more than they must.)
   auto issue_scales = [&](int kt) {
-    const int k = kstep(min(kt, nk - 1));
+    const int k = min(kt, nk - 1);
     if (k % S::GS == 0 && kt < nk) {
       if (wave < S::SROWS / 64)
         copy_to_lds_16(Sg + group_start(k), soff, lds0 + (uint32_t)(NS * S::STAGE + group_in * S::SCALES) + (uint32_t)wave * 1024u);
-      group_in = group_in + 1 == S::RING ? 0 : group_in + 1;
+      group_in ^= 1;
     }
   };
 
@@ -202,13 +199,11 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
     }
     const int owner = __builtin_ctzll(found);
     t.eg = a.lo + owner * 4 + __builtin_amdgcn_readlane(at, owner);
-    t.first_row = __builtin_amdgcn_readlane(vb, owner);
-    t.row0 = t.first_row + (mrow - __builtin_amdgcn_readlane(vf, owner)) * BM;
+    t.row0 = __builtin_amdgcn_readlane(vb, owner) + (mrow - __builtin_amdgcn_readlane(vf, owner)) * BM;
     t.rowEnd = __builtin_amdgcn_readlane(ve, owner);
     t.rows = min(BM, t.rowEnd - t.row0);
     t.tbv = min(S::TB, max(1, (((t.rows + 31) >> 5) - wm + S::WAVES_M - 1) / S::WAVES_M));
     t.n0 = nt * S::NOUT;
-    t.once = SINGLE && t.rowEnd - t.first_row <= BM;
     if (GATEUP && a.gather != nullptr) {
 #pragma unroll
       for (int i = 0; i < S::NLA; ++i) gathered[i] = a.gather[t.row0 + min((i * S::NW + wave) * 8 + crow, t.rows - 1)];
@@ -244,13 +239,9 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
       Sg = (GATEUP && w >= 2 ? a.B1s : a.B0s) + wrow * kb32;
       soff = (uint32_t)column((GATEUP ? w & 1 : w) * 64 + lane) * (uint32_t)kb32;
     }
-    // (whole groups of scales; with two groups in LDS none may be shorter than the others)
-    const unsigned groups = (unsigned)(nk + S::GS - 1) / S::GS;
-    krot = SINGLE && t.once && (S::RING > 2 || nk % S::GS == 0) ? (int)((unsigned)(eg * 5 + t.n0 / S::NOUT * 3) % groups) * S::GS : 0;
     for (int s = 0; s < NS; ++s) {
       issue_scales(s);
-      if (SINGLE && t.once) issue(s, s, number<0>{}, number<S::NL>{}, std::true_type{});
-      else issue(s, s, number<0>{}, number<S::NL>{}, std::false_type{});
+      issue(s, s, number<0>{}, number<S::NL>{});
     }
   };
 
@@ -272,7 +263,7 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
     // the step before, behind the barrier that publishes the step's stage.  That barrier also says that everybody has the step
     // before it in registers, so its buffer takes the copies of the stage NS steps ahead: a part in that slot, the rest in the
     // first two slots of the next step (at the first step they repeat copies of the prologue: the same bytes to the same place).
-    auto pipeline = [&](auto tbc_, auto once_) {
+    auto pipeline = [&](auto tbc_) {
       constexpr int TBc = decltype(tbc_)::value;
       constexpr int SLOTS = GATEUP ? 2 * TBc : 4;
       constexpr int PART0 = S::NL - 2 * (S::NL / 3), PART1 = SLOTS > 2 ? PART0 + S::NL / 3 : S::NL;
@@ -281,9 +272,9 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
       auto slot_copies = [&](auto s_, int kt, int st) {
         constexpr int s = decltype(s_)::value;
         const int before = st == 0 ? NS - 1 : st - 1;
-        if constexpr (s == SLOTS - 1) issue(kt + NS, st, number<0>{}, number<PART0>{}, once_);
-        if constexpr (s == 0) issue(kt - 1 + NS, before, number<PART0>{}, number<PART1>{}, once_);
-        if constexpr (s == 1 && SLOTS > 2) issue(kt - 1 + NS, before, number<PART1>{}, number<S::NL>{}, once_);
+        if constexpr (s == SLOTS - 1) issue(kt + NS, st, number<0>{}, number<PART0>{});
+        if constexpr (s == 0) issue(kt - 1 + NS, before, number<PART0>{}, number<PART1>{});
+        if constexpr (s == 1 && SLOTS > 2) issue(kt - 1 + NS, before, number<PART1>{}, number<S::NL>{});
       };
       auto publish = [&]() {                      // before a step's last slot
         wait_lds_reads();
@@ -294,11 +285,11 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
       // at the top of a step: the scales of the stage requested next, and where those of the next step (byte `scale_at` of each
       // row's 16, in LDS at `scales`) will be
       const unsigned char* scales = smem + NS * S::STAGE + group_out * S::SCALES;
-      int scale_at = S::SB * krot - group_start(krot);
+      int scale_at = -group_start(0);
       auto scales_top = [&](int kt) {
         issue_scales(kt + NS);
-        const int k = kstep(min(kt + 1, nk - 1));
-        if (kt + 1 < nk && k % S::GS == 0) group_out = group_out + 1 == S::RING ? 0 : group_out + 1;
+        const int k = min(kt + 1, nk - 1);
+        if (kt + 1 < nk && k % S::GS == 0) group_out ^= 1;
         scales = smem + NS * S::STAGE + group_out * S::SCALES;
         scale_at = S::SB * k - group_start(k);
       };
@@ -323,11 +314,12 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
         };
         auto read_scales = [&]() {
           const unsigned char* sc = scales + (scale_at & ~3);
+          const uint32_t scale_mask = scale_at == 14 ? 0xffffu : ~0u;
           auto one = [&](int row) -> uint32_t {
             const uint32_t lo = *reinterpret_cast<const uint32_t*>(sc + row * 16);
             if constexpr (!TAIL) return lo >> (8 * half);
             // (in the last group of a row of an odd number of pairs the step's bytes begin at an odd pair)
-            return __builtin_amdgcn_alignbit(*reinterpret_cast<const uint32_t*>(sc + row * 16 + 4), lo, (scale_at & 2) * 8) >> (8 * half);
+            return __builtin_amdgcn_alignbit(*reinterpret_cast<const uint32_t*>(sc + row * 16 + 4), lo, (scale_at & 2) * 8) >> (8 * half) & scale_mask;
           };
 #pragma unroll
           for (int nb = 0; nb < S::NB; ++nb) sw[nb] = one(BM + wrow(nb));
@@ -341,7 +333,7 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
           const unsigned char* base = smem + st * S::STAGE;
           const int st1 = st + 1 == NS ? 0 : st + 1;
           scales_top(kt);
-          const bool whole = !TAIL || kstep(kt) != nk - 1;
+          const uint32_t there = !TAIL || kt != nk - 1 ? ~0u : 0u;      // a step's second half
           for_range<0, SLOTS>([&](auto s_) {
             constexpr int s = decltype(s_)::value, m = s / TBc, tb = s % TBc;
             uint32_t sw0[S::NB], sx0 = sx[tb];
@@ -349,10 +341,17 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
             for (int nb = 0; nb < S::NB; ++nb) sw0[nb] = sw[nb];
             if constexpr (s == SLOTS - 1) publish();
             auto multiply = [&](int nb) {
+              if constexpr (TAIL && m == 1 && tb == 0) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  w[1][nb][0][i] &= there;
+                  w[1][nb][1][i] &= there;
+                }
+              }
               acc[nb][tb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(mx_operand(w[m][nb][0], w[m][nb][1]), mx_operand(x[s & 1][0], x[s & 1][1]),
                                                                             acc[nb][tb], 0, 0, 2 * m, (int)sw0[nb], 2 * m, (int)sx0);
             };
-            if (m == 0 || whole) multiply(0);
+            multiply(0);
             __builtin_amdgcn_sched_barrier(0x6);
             if constexpr (s < SLOTS - 1) {
               read_x(base, number<s + 1>{});
@@ -365,7 +364,7 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
             }
             slot_copies(s_, kt, st);
             __builtin_amdgcn_sched_barrier(0x6);
-            if (m == 0 || whole) multiply(1);
+            multiply(1);
             __builtin_amdgcn_sched_barrier(0x6);
           });
           st = st1;
@@ -426,20 +425,17 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
           st = st1;
         }
       }
-      group_out = group_out + 1 == S::RING ? 0 : group_out + 1;      // (the next tile begins a group)
+      group_out ^= 1;      // (the next tile begins a group)
       wait_lds_reads();
       wait_copies_but<0>();      // the repeated copies of the last steps: none may outlive the tile
       workgroup_barrier();       // the next tile's first copies overwrite stages that other waves may still read
     };
-    auto run_pipeline = [&](auto once_) {
-      switch (cur.tbv) {
-        case 1: pipeline(std::integral_constant<int, 1>{}, once_); break;
-        case 2: if constexpr (S::TB >= 2) pipeline(std::integral_constant<int, 2>{}, once_); break;
-        case 3: if constexpr (S::TB >= 3) pipeline(std::integral_constant<int, 3>{}, once_); break;
-        default: if constexpr (S::TB >= 4) pipeline(std::integral_constant<int, 4>{}, once_); break;
-      }
-    };
-    if (SINGLE && cur.once) run_pipeline(std::true_type{}); else run_pipeline(std::false_type{});
+    switch (cur.tbv) {
+      case 1: pipeline(number<1>{}); break;
+      case 2: if constexpr (S::TB >= 2) pipeline(number<2>{}); break;
+      case 3: if constexpr (S::TB >= 3) pipeline(number<3>{}); break;
+      default: if constexpr (S::TB >= 4) pipeline(number<4>{}); break;
+    }
 
     if constexpr (!EARLY) nxt = find_tile();
     request_tile(nxt);      // its first copies fly while this tile is stored
@@ -484,10 +480,10 @@ int num_cus() {
   return n;
 }
 
-template <int BM, bool GATEUP, int NS, bool TAIL, bool SINGLE>
+template <int BM, bool GATEUP, int NS, bool TAIL>
 int launch_tile_mx_t(const MxArgs& a, hipStream_t st) {
   using S = TileMxShape<BM, GATEUP, NS, TAIL>;
-  auto kern = expert_tile_mx_kernel<BM, GATEUP, NS, TAIL, SINGLE>;
+  auto kern = expert_tile_mx_kernel<BM, GATEUP, NS, TAIL>;
   constexpr int lds = S::LDS;
   if (a.Kdim < TILE_MX_MIN_K) return -2;
   static std::atomic<uint64_t> lds_raised{0};
@@ -502,12 +498,12 @@ int launch_tile_mx_t(const MxArgs& a, hipStream_t st) {
   return hipGetLastError() == hipSuccess ? 0 : -4;
 }
 
-template <int BM, bool GATEUP, int NS, bool SINGLE>
+template <int BM, bool GATEUP, int NS>
 int launch_tile_mx_any(const MxArgs& a, hipStream_t st) {
   if constexpr (GATEUP) {
-    if (a.Kdim % 128 != 0) return launch_tile_mx_t<BM, true, NS, true, SINGLE>(a, st);
+    if (a.Kdim % 128 != 0) return launch_tile_mx_t<BM, true, NS, true>(a, st);
   }
-  return launch_tile_mx_t<BM, GATEUP, NS, false, SINGLE>(a, st);
+  return launch_tile_mx_t<BM, GATEUP, NS, false>(a, st);
 }
 
 // Tile height from the layer-wide mean (never from the block bounds).
@@ -520,16 +516,16 @@ int tile_height(const MxArgs& a) {
 
 int launch_tile_mx_gateup(const MxArgs& a, hipStream_t st) {
   switch (tile_height(a)) {
-    case 64: return launch_tile_mx_any<64, true, 3, true>(a, st);
-    case 128: return launch_tile_mx_any<128, true, 3, true>(a, st);
-    default: return launch_tile_mx_any<256, true, 2, false>(a, st);
+    case 64: return launch_tile_mx_any<64, true, 3>(a, st);
+    case 128: return launch_tile_mx_any<128, true, 3>(a, st);
+    default: return launch_tile_mx_any<256, true, 2>(a, st);
   }
 }
 int launch_tile_mx_down(const MxArgs& a, hipStream_t st) {
   switch (tile_height(a)) {
-    case 64: return launch_tile_mx_any<64, false, 5, true>(a, st);
-    case 128: return launch_tile_mx_any<128, false, 4, true>(a, st);
-    default: return launch_tile_mx_any<256, false, 3, false>(a, st);
+    case 64: return launch_tile_mx_any<64, false, 5>(a, st);
+    case 128: return launch_tile_mx_any<128, false, 4>(a, st);
+    default: return launch_tile_mx_any<256, false, 3>(a, st);
   }
 }
 
