@@ -64,8 +64,10 @@ struct MxArgs {
 };
 int launch_stream_mx_gateup(const MxArgs& a, hipStream_t st);
 int launch_stream_mx_down(const MxArgs& a, hipStream_t st);
-// Tiles: more than 32 rows per expert, and a contraction long enough for their scales to come 16 bytes of a row at a time.
-inline bool mx_in_tiles(const MxArgs& a) { return a.mean_rows > 32 && a.Kdim >= 512; }
+// Tiles: more than 24 rows per expert, and a contraction long enough for their scales to come 16 bytes of a row at a time.
+// (60 experts, H 2048, I 1408, gate/up + down, tiles and streamed: 17 rows 75 + 45 and 72 + 42 us, 27 rows 76 + 46 and 80 + 47,
+// 40 rows 78 + 48 and 128 + 65.)
+inline bool mx_in_tiles(const MxArgs& a) { return a.mean_rows > 24 && a.Kdim >= 512; }
 int launch_tile_mx_gateup(const MxArgs& a, hipStream_t st);
 int launch_tile_mx_down(const MxArgs& a, hipStream_t st);
 
