@@ -14,6 +14,10 @@
 // (Weights come from the logits at hand, whose last bits are either evaluation's.)  About one token in forty is looked at
 // twice (256 experts in 8 groups, H 2048).
 //
+// Measured (H 2048): 13 tokens, 60 experts 9.4 us, 3 of them the products and 4 the choice; 301 tokens, 256 experts in 8 groups
+// 29 us (8 products: every workgroup reads the router's 1 MB; 2.5 their sum; 7 the choice, and 9 more where near ties are
+// formed again); 8192 such tokens 49 us (15 + 5 + 9, and up to 17); 16 384 tokens, 60 experts, sigmoid 33 us.
+//
 // The bound: one 16x16x32 step is off by at most 6 * 2^-24 of the sum of its terms' magnitudes (measured, products over 18
 // orders of magnitude among them), whole logits of H 2048 by 1.3 * 2^-24 of theirs, and the defined order by less; assumed
 // are 32 * 2^-24 (beyond H 2048 H / 64 * 2^-24) of |x[t]| * max_e |Wr[e]|, which is more than that sum.
@@ -36,8 +40,8 @@ __device__ __forceinline__ float key_value(uint32_t k) {
 }
 __device__ __forceinline__ double sigmoid64(float l) { return 1.0 / (1.0 + exp(-(double)l)); }
 
-// Folds over a row of 16 lanes; every lane has the result
-template <class T, class F>
+// Folds over a row of LANES (16 or 32) lanes; every lane has the result
+template <int LANES, class T, class F>
 __device__ __forceinline__ T row_fold(T v, F&& f) {
   auto other = [](T x, auto ctrl) {
     return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xF, 0xF, false));
@@ -45,12 +49,23 @@ __device__ __forceinline__ T row_fold(T v, F&& f) {
   v = f(v, other(v, std::integral_constant<int, 0xB1>{}));
   v = f(v, other(v, std::integral_constant<int, 0x4E>{}));
   v = f(v, other(v, std::integral_constant<int, 0x141>{}));
-  return f(v, other(v, std::integral_constant<int, 0x140>{}));
+  v = f(v, other(v, std::integral_constant<int, 0x140>{}));
+  if constexpr (LANES == 32) {
+    const uint32_t bits = __builtin_bit_cast(uint32_t, v);
+    const auto both = __builtin_amdgcn_permlane16_swap(bits, bits, false, false);      // the even 16 lanes' value, and the odd ones'
+    const uint32_t even = both[0], odd = both[1];
+    v = f(__builtin_bit_cast(T, even), __builtin_bit_cast(T, odd));
+  }
+  return v;
 }
-__device__ __forceinline__ uint32_t row_max(uint32_t v) { return row_fold(v, [](uint32_t a, uint32_t b) { return max(a, b); }); }
-__device__ __forceinline__ uint32_t row_min(uint32_t v) { return row_fold(v, [](uint32_t a, uint32_t b) { return min(a, b); }); }
-__device__ __forceinline__ float row_max(float v) { return row_fold(v, [](float a, float b) { return fmaxf(a, b); }); }
-__device__ __forceinline__ float row_sum(float v) { return row_fold(v, [](float a, float b) { return a + b; }); }
+template <int LANES>
+__device__ __forceinline__ uint32_t row_max(uint32_t v) { return row_fold<LANES>(v, [](uint32_t a, uint32_t b) { return max(a, b); }); }
+template <int LANES>
+__device__ __forceinline__ uint32_t row_min(uint32_t v) { return row_fold<LANES>(v, [](uint32_t a, uint32_t b) { return min(a, b); }); }
+template <int LANES>
+__device__ __forceinline__ float row_max(float v) { return row_fold<LANES>(v, [](float a, float b) { return fmaxf(a, b); }); }
+template <int LANES>
+__device__ __forceinline__ float row_sum(float v) { return row_fold<LANES>(v, [](float a, float b) { return a + b; }); }
 
 // N logits by one wave, of token rows x[n] (or one for all) and router rows w[n], in the defined order.  Four chunks of 512 at a time
 // are requested before they are used.
@@ -87,84 +102,92 @@ __device__ __forceinline__ void defined_logits(const bf16_t* const (&x)[NX], con
 
 constexpr int GROUPS_MAX = 64;
 
-// Four tokens by one wave, one per row of 16 lanes; lane j of a row owns experts EPL j .. EPL j + EPL - 1.  What belongs to a token
-// is the same in the 16 lanes of its row.
-//   t, want: the token and whether its row of results is asked for;  whole: its logits are the defined ones;
+// 64 / LANES tokens by one wave, one per row of LANES lanes; lane j of a row owns experts EPL j .. EPL j + EPL - 1.  What belongs to
+// a token is the same in the lanes of its row.
+//   t, want: the token and whether its row of results is asked for;  whole: the logits are the defined ones (in all rows);
 //   s_logit: its logits in LDS (by expert; exact ones are written back);  s_bal: the balance, by expert, at most bal_most;
-//   doubt: what a logit may be off by, negative if that is not known;  s_key, s_thr: EPL * 16 and 64 words of the row.
+//   doubt: what a logit may be off by, negative if that is not known;  s_key, s_thr: EPL * LANES and 64 words of the row.
 // True where the choice cannot be made without all of the token's logits in the defined order; then nothing is written.
-template <int EPL>
+template <int EPL, int LANES>
 __device__ __forceinline__ bool choose(const RouteScored& a, int t, bool want, bool whole, float* s_logit, const float* s_bal, float bal_most,
                                        float doubt, int lane, uint32_t* s_key, float* s_thr) {
-  const int j16 = lane & 15, e0 = EPL * j16;
+  static_assert(LANES == 16 || LANES == 32, "rows");
+  const int jl = lane & (LANES - 1), row0 = lane & (64 - LANES), e0 = EPL * jl;
   const int size = a.E / a.groups;
   const uint32_t per_group = 65536u / (uint32_t)size + 1u;                   // e / size = e * per_group >> 16 for e < 256
+  auto group_of = [&](int e) { return __umul24((uint32_t)e, per_group) >> 16; };
   const bool grouped = a.groups > a.top_groups;
   // softmax without extras orders like its logits
   const bool by_logit = !whole && !a.sigmoid && a.balance == nullptr && (!grouped || a.best == 1);
-  auto row_any = [&](bool v) { return ((__ballot(v) >> (lane & 48)) & 0xffffull) != 0ull; };
+  auto row_any = [&](bool v) { return ((__ballot(v) >> row0) & ((1ull << LANES) - 1ull)) != 0ull; };
 
   uint32_t key[EPL];         // what is compared, 0 beyond E
   float m = 0.0f, share = 0.0f;
   double z = 1.0;
-  unsigned exact = 0u;       // this lane's experts whose logit (and key) is the defined one
+  unsigned exact = whole ? ~0u : 0u;       // this lane's experts whose logit (and key) is the defined one
   bool redo = false;
   {
     float l[EPL];
 #pragma unroll
-    for (int i = 0; i < EPL; i += 4) {
-      const f32x4 v = *reinterpret_cast<const f32x4*>(s_logit + e0 + i);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) l[i + j] = e0 + i + j < a.E ? v[j] : 0.0f;
+    for (int i = 0; i < EPL; i += 2) {
+      const float2 v = *reinterpret_cast<const float2*>(s_logit + e0 + i);
+      l[i] = e0 + i < a.E ? v.x : 0.0f;
+      l[i + 1] = e0 + i + 1 < a.E ? v.y : 0.0f;
     }
-    float magnitudes = 0.0f, top = -INFINITY;
+    float magnitudes = 0.0f;
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) {
-      magnitudes += fabsf(l[i]);
-      if (e0 + i < a.E) top = fmaxf(top, l[i]);
-    }
+    for (int i = 0; i < EPL; ++i) magnitudes += fabsf(l[i]);
     if (row_any(magnitudes != 0.0f)) redo = !whole && (doubt < 0.0f || row_any(!(magnitudes < INFINITY)));
     else doubt = 0.0f;       // (a row of zeros: 0 in any order)
-    if (!a.sigmoid) m = row_max(top);
-    if (__any(whole)) {      // scores in 64 bits
-      double sum = 0.0;
+    if (!a.sigmoid) {
+      float top = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) top = e0 + i < a.E ? fmaxf(top, l[i]) : top;
+      m = row_max<LANES>(top);
+    }
+    if (whole) {             // scores in 64 bits
       if (!a.sigmoid) {
+        double sum = 0.0;
 #pragma unroll 1
         for (int i = 0; i < EPL; ++i)
           if (e0 + i < a.E) sum += exp((double)s_logit[e0 + i] - (double)m);
 #pragma unroll
-        for (int w = 1; w < 16; w <<= 1) sum += __shfl_xor(sum, w, WAVE);
+        for (int w = 1; w < LANES; w <<= 1) sum += __shfl_xor(sum, w, WAVE);
+        z = sum;
       }
 #pragma unroll 1
       for (int i = 0; i < EPL; ++i) {
         const double v = (double)s_logit[e0 + i];
-        s_key[e0 + i] = __float_as_uint((float)(a.sigmoid ? 1.0 / (1.0 + exp(-v)) : exp(v - (double)m) / sum));
+        s_key[e0 + i] = __float_as_uint((float)(a.sigmoid ? 1.0 / (1.0 + exp(-v)) : exp(v - (double)m) / z));
       }
-      if (whole) {
-        z = sum;
-        exact = ~0u;
-      }
-    }
-    if (a.sigmoid) {
 #pragma unroll
-      for (int i = 0; i < EPL; ++i) l[i] = whole ? __uint_as_float(s_key[e0 + i]) : __fdividef(1.0f, 1.0f + __expf(-l[i]));
+      for (int i = 0; i < EPL; ++i) l[i] = __uint_as_float(s_key[e0 + i]);
+    } else if (a.sigmoid) {
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) l[i] = __fdividef(1.0f, 1.0f + __expf(-l[i]));
     } else if (!by_logit) {
       float sum = 0.0f;
 #pragma unroll
       for (int i = 0; i < EPL; ++i) {
-        l[i] = whole ? __uint_as_float(s_key[e0 + i]) : e0 + i < a.E ? expf(l[i] - m) : 0.0f;
+        l[i] = e0 + i < a.E ? expf(l[i] - m) : 0.0f;
         sum += l[i];
       }
-      sum = row_sum(sum);
-      if (!whole) {
-        z = sum;
-        share = 2.1f * doubt + 4e-6f;
+      sum = row_sum<LANES>(sum);
+      z = sum;
+      share = 2.1f * doubt + 4e-6f;
 #pragma unroll
-        for (int i = 0; i < EPL; ++i) l[i] = l[i] / sum;
+      for (int i = 0; i < EPL; ++i) l[i] = l[i] / sum;
+    }
+    if (a.balance != nullptr) {
+#pragma unroll
+      for (int i = 0; i < EPL; i += 2) {
+        const float2 v = *reinterpret_cast<const float2*>(s_bal + e0 + i);
+        l[i] += v.x;
+        l[i + 1] += v.y;
       }
     }
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) key[i] = e0 + i < a.E ? order_key(a.balance != nullptr ? l[i] + s_bal[e0 + i] : l[i]) : 0u;
+    for (int i = 0; i < EPL; ++i) key[i] = e0 + i < a.E ? order_key(l[i]) : 0u;
   }
   // what a compared value of magnitude c may be off by
   const float own = a.sigmoid ? 0.25f * doubt + 2e-6f : by_logit ? doubt : 0.0f, largest = 1.0f / (float)z;
@@ -181,58 +204,67 @@ __device__ __forceinline__ bool choose(const RouteScored& a, int t, bool want, b
     for (int i = 0; i < EPL; ++i) cur[i] = key[i];
 
     if (grouped) {
-      // lane j of a row takes groups j, j + 16, ..: their two largest keys, then the best groups one by one
+      // lane j of a row takes groups j, j + LANES, ..: their two largest keys, then the best groups one by one
 #pragma unroll
-      for (int i = 0; i < EPL; i += 4) *reinterpret_cast<u32x4*>(s_key + e0 + i) = u32x4{key[i], key[i + 1], key[i + 2], key[i + 3]};
+      for (int i = 0; i < EPL; i += 2) *reinterpret_cast<uint2*>(s_key + e0 + i) = uint2{key[i], key[i + 1]};
       __builtin_amdgcn_wave_barrier();
-      uint32_t value[4], left[4];
-      float low[4], size_of[4];    // the smallest c that counts in a group's value, and how large those are
+      constexpr int GPL = GROUPS_MAX / LANES;
+      uint32_t value[GPL], left[GPL];
+      float low[GPL], size_of[GPL];    // the smallest c that counts in a group's value, and how large those are
 #pragma unroll
-      for (int gi = 0; gi < 4; ++gi) {
+      for (int gi = 0; gi < GPL; ++gi) {
         value[gi] = left[gi] = 0u;
         low[gi] = size_of[gi] = 0.0f;
-        const int g = j16 + 16 * gi;
-        if (16 * gi < a.groups && g < a.groups) {
+        const int g = jl + LANES * gi;
+        if (LANES * gi < a.groups && g < a.groups) {
           uint32_t k1 = 0u, k2 = 0u;
           auto take = [&](uint32_t k) {
             k2 = max(k2, min(k1, k));
             k1 = max(k1, k);
           };
-          int j = 0;
-          if ((size & 3) == 0) {
+          if ((size & 3) == 0) {       // (each group from a place of its own on: other LDS banks)
+            int at = 4 * (g % (size / 4));
 #pragma unroll 4
-            for (; j < size; j += 4) {
-              const u32x4 k = *reinterpret_cast<const u32x4*>(s_key + g * size + j);
+            for (int j = 0; j < size; j += 4) {
+              const u32x4 k = *reinterpret_cast<const u32x4*>(s_key + g * size + at);
               take(k.x); take(k.y); take(k.z); take(k.w);
+              at = at + 4 == size ? 0 : at + 4;
             }
+          } else {
+            for (int j = 0; j < size; ++j) take(s_key[g * size + j]);
           }
-          for (; j < size; ++j) take(s_key[g * size + j]);
           const float v1 = key_value(k1), v2 = key_value(k2);
           value[gi] = left[gi] = a.best == 1 ? k1 : order_key(v1 + v2);
           low[gi] = a.best == 1 ? v1 : v2;
           size_of[gi] = fabsf(v1) + (a.best == 1 ? 0.0f : fabsf(v2));
         }
       }
+      auto most_left = [&]() {
+        uint32_t v = left[0];
+#pragma unroll
+        for (int gi = 1; gi < GPL; ++gi) v = max(v, left[gi]);
+        return row_max<LANES>(v);
+      };
       __builtin_amdgcn_wave_barrier();
       uint32_t last = 0u;
       unsigned long long kept = 0ull;
       for (int j = 0; j < a.top_groups; ++j) {
-        last = row_max(max(max(left[0], left[1]), max(left[2], left[3])));
+        last = most_left();
         uint32_t g = GROUPS_MAX;
 #pragma unroll
-        for (int gi = 3; gi >= 0; --gi)
-          if (left[gi] == last) g = j16 + 16 * gi;                           // (last is not 0: more groups than are kept)
-        g = row_min(g);
+        for (int gi = GPL - 1; gi >= 0; --gi)
+          if (left[gi] == last) g = jl + LANES * gi;                        // (last is not 0: more groups than are kept)
+        g = row_min<LANES>(g);
         kept |= 1ull << g;
 #pragma unroll
-        for (int gi = 0; gi < 4; ++gi) left[gi] = j16 + 16 * gi == (int)g ? 0u : left[gi];
+        for (int gi = 0; gi < GPL; ++gi) left[gi] = jl + LANES * gi == (int)g ? 0u : left[gi];
       }
       // the border between the last group kept and the best one left: who may be on either side of it
-      const float vk = key_value(last), vn = key_value(row_max(max(max(left[0], left[1]), max(left[2], left[3]))));
+      const float vk = key_value(last), vn = key_value(most_left());
       bool close = false;
-      float thr[4];
+      float thr[GPL];
 #pragma unroll
-      for (int gi = 0; gi < 4; ++gi) {
+      for (int gi = 0; gi < GPL; ++gi) {
         const float v = key_value(value[gi]);
         const float moved = 2.0f * a.best * off(0.5f * size_of[gi]) + 1e-6f * size_of[gi];      // two values, of one or two c each
         const bool in = !whole && value[gi] != 0u && size_of[gi] < INFINITY && vk - vn <= moved && v >= vk - moved && v <= vn + moved;
@@ -241,19 +273,19 @@ __device__ __forceinline__ bool choose(const RouteScored& a, int t, bool want, b
       }
       if (__any(close)) {
 #pragma unroll
-        for (int gi = 0; gi < 4; ++gi) s_thr[j16 + 16 * gi] = thr[gi];
+        for (int gi = 0; gi < GPL; ++gi) s_thr[jl + LANES * gi] = thr[gi];
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int i = 0; i < EPL; ++i) {
           const float c = key_value(key[i]);
-          if (key[i] != 0u && ((exact >> i) & 1u) == 0u && fabsf(c) < INFINITY && c >= s_thr[(uint32_t)(e0 + i) * per_group >> 16]) again |= 1u << i;
+          if (key[i] != 0u && ((exact >> i) & 1u) == 0u && fabsf(c) < INFINITY && c >= s_thr[group_of(e0 + i)]) again |= 1u << i;
         }
         __builtin_amdgcn_wave_barrier();
       }
       if (by_logit) alike = (vk != vn && vk - vn <= 2e-6f * fmaxf(1.0f, fabsf(vk))) || vk - m < -70.0f;
       else if (!a.sigmoid) alike = close;
 #pragma unroll
-      for (int i = 0; i < EPL; ++i) cur[i] = (kept >> ((uint32_t)(e0 + i) * per_group >> 16)) & 1ull ? cur[i] : 0u;
+      for (int i = 0; i < EPL; ++i) cur[i] = (kept >> group_of(e0 + i)) & 1ull ? cur[i] : 0u;
     }
     unsigned allowed = 0u;
 #pragma unroll
@@ -263,49 +295,55 @@ __device__ __forceinline__ bool choose(const RouteScored& a, int t, bool want, b
       uint32_t k = cur[0];
 #pragma unroll
       for (int i = 1; i < EPL; ++i) k = max(k, cur[i]);
-      return row_max(k);
+      return row_max<LANES>(k);
     };
-    float my_c = 0.0f, before = __uint_as_float(0x7fc00000u), s_before = 0.0f, most = 0.0f;
-    bool close = false;
-    auto compare = [&](float c, int e) {     // with the one chosen before it (a NaN or an infinite one is what it is)
-      const float d = before - c, large = fmaxf(fabsf(before), fabsf(c));
-      const bool both = large < INFINITY;
-      close |= both && d <= 2.0f * off(large);
-      most = both ? fmaxf(most, large) : most;
-      if (by_logit) {
-        alike |= both && d > 0.0f && d <= 4e-7f * fmaxf(1.0f, large);
-      } else if (!a.sigmoid) {               // between exact logits what is left is the denominator's error
-        const float sc = a.balance != nullptr ? c - s_bal[e] : c;
-        alike |= both && d <= 2.1f * doubt * fabsf(s_before - sc) + 5e-7f * (large + fabsf(sc));
-        s_before = sc;
-      }
-      before = c;
-    };
-    float next = __uint_as_float(0x7fc00000u);     // the border: the best one that is not chosen
-    for (int j = 0; j <= a.K; ++j) {         // (the last one is not chosen: the border)
-      const uint32_t k = best_left();
+    auto expert_of = [&](uint32_t k) {       // the first one left with this key
       uint32_t e = 256u;
 #pragma unroll
-      for (int i = EPL - 1; i >= 0; --i)
-        if (cur[i] == k) e = (uint32_t)(e0 + i);
-      e = row_min(e);
-      const float c = key_value(k);
-      if (k != 0u) compare(c, (int)e);       // (no expert is left only behind the last choice)
-      if (j == a.K) {
-        next = c;
-        break;
-      }
+      for (int i = EPL - 1; i >= 0; --i) e = cur[i] == k ? (uint32_t)(e0 + i) : e;
+      return (int)row_min<LANES>(e);
+    };
+    uint32_t my_key = 0u;                    // lane j < K: the j-th choice
+    for (int j = 0; j < a.K; ++j) {
+      const uint32_t k = best_left();
+      const int e = expert_of(k);
 #pragma unroll
-      for (int i = 0; i < EPL; ++i) cur[i] = e == (uint32_t)(e0 + i) ? 0u : cur[i];
-      if (by_logit) alike |= c - m < -70.0f;
-      if (j16 == j) { my_id = (int)e; my_c = c; }
+      for (int i = 0; i < EPL; ++i) cur[i] = e == e0 + i ? 0u : cur[i];
+      my_key = jl == j ? k : my_key;
+      my_id = jl == j ? e : my_id;
     }
-    close = close && !whole;
+    const uint32_t border = best_left();     // the best one that is not chosen (none is left: 0)
+    const float my_c = key_value(my_key), next = key_value(border);
+    bool close;
+    float most;
+    {
+      // every choice with the one after it, the last with the border (a NaN or an infinite one is what it is)
+      auto following = [&](float v, float last) {
+        const float w = __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x101, 0xF, 0xF, false));     // row_shl 1
+        return jl == a.K - 1 ? last : w;
+      };
+      const float after = following(my_c, next), d = my_c - after, large = fmaxf(fabsf(my_c), fabsf(after));
+      const bool both = (jl < a.K - 1 || (jl == a.K - 1 && border != 0u)) && large < INFINITY;
+      close = both && d <= 2.0f * off(large);
+      most = row_max<LANES>(fmaxf(jl < a.K && fabsf(my_c) < INFINITY ? fabsf(my_c) : 0.0f, fabsf(next) < INFINITY ? fabsf(next) : 0.0f));
+      if (by_logit) {
+        alike |= (both && d > 0.0f && d <= 4e-7f * fmaxf(1.0f, large)) || (jl < a.K && my_c - m < -70.0f);
+      } else if (!a.sigmoid) {               // between exact logits what is left is the denominator's error
+        float score = my_c, score_next = next;
+        if (a.balance != nullptr) {
+          score -= s_bal[my_id];
+          score_next -= s_bal[min(expert_of(border), a.E - 1)];
+        }
+        const float s_after = following(score, score_next);
+        alike |= both && d <= 2.1f * doubt * fabsf(score - s_after) + 5e-7f * (large + fabsf(s_after));
+      }
+    }
+    close = !whole && row_any(close);
     if (__any(close)) {      // whose logits lie that near to another's, at or above the border of the choice
       const float width = 2.0f * off(most);
       unsigned one = 0u, two = 0u;           // experts with a chosen value, or two, that near (a chosen one's own counts)
       for (int j = 0; j <= a.K; ++j) {
-        const float c = j < a.K ? __shfl(my_c, (lane & 48) + j, WAVE) : next;
+        const float c = j < a.K ? __shfl(my_c, row0 + j, WAVE) : next;
         unsigned hit = 0u;
 #pragma unroll
         for (int i = 0; i < EPL; ++i) hit |= fabsf(key_value(key[i]) - c) <= width ? 1u << i : 0u;
@@ -343,12 +381,12 @@ __device__ __forceinline__ bool choose(const RouteScored& a, int t, bool want, b
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
         xs[n] = a.x + (size_t)__builtin_amdgcn_readlane(t, at[n]) * a.H;
-        ws[n] = a.Wr + (size_t)(EPL * (at[n] & 15) + slot[n]) * a.H;
+        ws[n] = a.Wr + (size_t)(EPL * (at[n] & (LANES - 1)) + slot[n]) * a.H;
       }
       defined_logits(xs, ws, a.H, lane, v);
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
-        const int e = EPL * (at[n] & 15) + slot[n];
+        const int e = EPL * (at[n] & (LANES - 1)) + slot[n];
         const float score = a.sigmoid ? (float)sigmoid64(v[n]) : by_logit ? v[n] : (float)(exp((double)v[n] - (double)m) / z);
         const uint32_t k = order_key(a.balance != nullptr ? score + s_bal[e] : score);     // (of the owner's token: the owner's)
         if (lane == at[n]) {
@@ -364,17 +402,17 @@ __device__ __forceinline__ bool choose(const RouteScored& a, int t, bool want, b
     float sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < EPL; ++i) sum += e0 + i < a.E ? expf(s_logit[e0 + i] - m) : 0.0f;
-    z = row_sum(sum);
+    z = row_sum<LANES>(sum);
   }
   float s = 0.0f;
-  if (j16 < a.K) {
+  if (jl < a.K) {
     const float l = s_logit[my_id];
     s = a.sigmoid ? 1.0f / (1.0f + expf(-l)) : expf(l - m) / (float)z;
   }
-  if (a.renorm) s = s / (row_sum(s) + 1e-20f);
-  if (j16 < a.K && want && !redo) {
-    a.ids[(size_t)t * a.K + j16] = my_id;
-    a.w[(size_t)t * a.K + j16] = s * a.scale;
+  if (a.renorm) s = s / (row_sum<LANES>(s) + 1e-20f);
+  if (jl < a.K && want && !redo) {
+    a.ids[(size_t)t * a.K + jl] = my_id;
+    a.w[(size_t)t * a.K + jl] = s * a.scale;
   }
   return redo;
 }
@@ -385,10 +423,13 @@ __device__ __forceinline__ bool choose(const RouteScored& a, int t, bool want, b
 // as operands from there.  (Loaded as operands, 16 rows by 16 bytes per 16 lanes, they took four times as long: 0.35 us per
 // block and wave, of the address unit.)  The eight partial sums meet in LDS, eight tiles at a time, and are added in the order
 // of the parts: a logit's bits depend on H alone.  The squares for the error bound are summed from the same operands.
+// The choice is a chain of small steps, bound by their latency: all eight waves share the tokens, 32 lanes for each of 16 (half as
+// many experts per lane as with 16 lanes: 301 tokens 29 us, with 16 lanes and half of the waves idle 33), 16 lanes for each of 32.
 constexpr int ROUTE_WAVES = 8, ROUTE_RING = 8;                               // items of 2 KB in a wave's ring
 template <int NBLK, int TT>
 struct RouteShape {
   static constexpr int TOKENS = 16 * TT, EP = 16 * NBLK, LDL = EP + 4;       // logits [TOKENS][LDL]
+  static constexpr int LANES = 64 * ROUTE_WAVES / TOKENS;                    // that choose for a token
   static constexpr int RINGS = ROUTE_WAVES * ROUTE_RING * 2048;              // then: parts (later keys and thresholds), logits behind them
   static constexpr int PARTS = ROUTE_WAVES * 8 * 1024, LOGITS = TOKENS * LDL * 4, NORMS = ROUTE_WAVES * 4 * (1 + TOKENS) * 4, BAL = EP * 4;
   static constexpr int LDS = RINGS + NORMS + BAL;
@@ -486,7 +527,7 @@ __global__ __launch_bounds__(64 * ROUTE_WAVES) void route_scored_kernel(RouteSco
   float wpart = wn[0];
 #pragma unroll
   for (int b = 1; b < NBLK; ++b) wpart = fmaxf(wpart, wn[b]);
-  wpart = row_max(wpart);
+  wpart = row_max<16>(wpart);
   if (r16 == 0) s_wn[wave * 4 + g] = wpart;
 #pragma unroll
   for (int tt = 0; tt < TT; ++tt) s_xn[(16 * tt + r16) * (ROUTE_WAVES * 4) + wave * 4 + g] = xn[tt];
@@ -517,21 +558,20 @@ __global__ __launch_bounds__(64 * ROUTE_WAVES) void route_scored_kernel(RouteSco
     for (int e = lane; e < S::EP; e += 64) bal_most = fmaxf(bal_most, fabsf(s_bal[e]) < INFINITY ? fabsf(s_bal[e]) : 0.0f);
     bal_most = fold_max(bal_most);
   }
-  const int tk = (wave * 4 + (lane >> 4)) % S::TOKENS, t = t0 + tk;          // (waves without tokens of their own help out only)
-  const float w2 = row_sum(s_wn[r16] + s_wn[16 + r16]), x2 = row_sum(s_xn[tk * 32 + r16] + s_xn[tk * 32 + 16 + r16]);
+  const int tk = (wave * 64 + lane) / S::LANES, t = t0 + tk;
+  const float w2 = row_sum<16>(s_wn[r16] + s_wn[16 + r16]), x2 = row_sum<16>(s_xn[tk * 32 + r16] + s_xn[tk * 32 + 16 + r16]);
   const bool known = x2 >= 1e-30f && x2 < INFINITY && w2 >= 1e-30f && w2 < INFINITY;     // (squares that did not vanish or overflow)
   uint32_t* const s_key = reinterpret_cast<uint32_t*>(smem) + tk * (S::EP + GROUPS_MAX);
   const float doubt = known ? LOGIT_ERROR * fmaxf(1.0f, (float)H / 2048.0f) * sqrtf(x2) * sqrtf(w2) : -1.0f;
   int* const s_redo = reinterpret_cast<int*>(s_wn);                          // (every wave has read the norms before the barrier below)
   bool redo = false;
   for (int pass = 0; pass < 2; ++pass) {
-    if (wave * 4 < S::TOKENS)
-      redo = choose<NBLK>(a, min(t, a.T - 1), t < a.T && (pass == 0 || redo), pass > 0 && redo, s_logit + tk * S::LDL, s_bal, bal_most, doubt,
-                          lane, s_key, reinterpret_cast<float*>(s_key + S::EP)) && t < a.T;
+    redo = choose<S::EP / S::LANES, S::LANES>(a, min(t, a.T - 1), t < a.T && (pass == 0 || redo), pass > 0, s_logit + tk * S::LDL, s_bal,
+                                              bal_most, doubt, lane, s_key, reinterpret_cast<float*>(s_key + S::EP)) && t < a.T;
     if (pass > 0 || !__syncthreads_or(redo)) break;
     // the tokens that need all of their logits in the defined order (values that are not finite, softmax scores too close to
     // tell apart by a denominator that is not exact): by all waves
-    if (r16 == 0 && wave * 4 < S::TOKENS) s_redo[tk] = redo;
+    if ((lane & (S::LANES - 1)) == 0) s_redo[tk] = redo;
     __syncthreads();
     for (int i = 0; i < S::TOKENS; ++i) {
       if (s_redo[i] == 0) continue;
