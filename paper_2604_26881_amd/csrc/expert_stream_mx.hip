@@ -294,7 +294,7 @@ __global__ __launch_bounds__(256) void expert_stream_mx_kernel(MxArgs a) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       v[j] = total(c + j, m);
-      if (GATEUP) v[j] = __fdividef(v[j], 1.0f + __expf(-v[j])) * total(S::WROWS / 2 + c + j, m);
+      if (GATEUP) v[j] = silu_times(v[j], total(S::WROWS / 2 + c + j, m));
     }
     *reinterpret_cast<uint2*>(a.C + (size_t)(rb + m0 + m) * N + n0 + c) = uint2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
   }

@@ -70,7 +70,6 @@ template <int BM, bool GATEUP, int NS, bool TAIL>
 __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
   using S = TileMxShape<BM, GATEUP, NS, TAIL>;
   extern __shared__ __align__(16) unsigned char smem[];
-  constexpr bool EARLY = BM < 256;
   constexpr int HEAVY_MIN = 3;       // token tiles from which an expert counts as bound by the matrix cores
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -248,8 +247,7 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
   Tile cur = find_tile();
   request_tile(cur);
   while (cur.valid) {
-    Tile nxt;
-    if constexpr (EARLY) nxt = find_tile();
+    const Tile nxt = find_tile();
     f32x16 acc[S::NB][S::TB];
 #pragma unroll
     for (int nb = 0; nb < S::NB; ++nb)
@@ -437,7 +435,6 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
       default: if constexpr (S::TB >= 4) pipeline(number<4>{}); break;
     }
 
-    if constexpr (!EARLY) nxt = find_tile();
     request_tile(nxt);      // its first copies fly while this tile is stored
 
     // accumulator element i of block (nb, tb): column 8 (i / 4) + 4 half + i % 4 of the block, token row lane % 32; lanes l and
@@ -457,7 +454,7 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
 #pragma unroll
               for (int i = 0; i < 8; ++i) {
                 const float g = acc[nb][tb][4 * q + i];
-                v[i] = GATEUP ? __fdividef(g, 1.0f + __expf(-g)) * acc[S::NB - 1][tb][4 * q + i] : g;
+                v[i] = GATEUP ? silu_times(g, acc[S::NB - 1][tb][4 * q + i]) : g;
               }
               uint32_t ox = pack_bf16x2(v[0], v[1]), oy = pack_bf16x2(v[2], v[3]);
               uint32_t oz = pack_bf16x2(v[4], v[5]), ow = pack_bf16x2(v[6], v[7]);

@@ -164,7 +164,7 @@ __device__ __forceinline__ bool choose(const RouteScored& a, int t, bool want, b
       for (int i = 0; i < EPL; ++i) l[i] = __uint_as_float(s_key[e0 + i]);
     } else if (a.sigmoid) {
 #pragma unroll
-      for (int i = 0; i < EPL; ++i) l[i] = __fdividef(1.0f, 1.0f + __expf(-l[i]));
+      for (int i = 0; i < EPL; ++i) l[i] = __builtin_amdgcn_rcpf(1.0f + __expf(-l[i]));
     } else if (!by_logit) {
       float sum = 0.0f;
 #pragma unroll
@@ -175,8 +175,9 @@ __device__ __forceinline__ bool choose(const RouteScored& a, int t, bool want, b
       sum = row_sum<LANES>(sum);
       z = sum;
       share = 2.1f * doubt + 4e-6f;
+      const float inverse = 1.0f / sum;
 #pragma unroll
-      for (int i = 0; i < EPL; ++i) l[i] = l[i] / sum;
+      for (int i = 0; i < EPL; ++i) l[i] *= inverse;
     }
     if (a.balance != nullptr) {
 #pragma unroll
