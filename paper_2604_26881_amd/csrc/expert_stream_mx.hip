@@ -21,7 +21,7 @@
 // pieces would be half as many bytes as the weights).
 // The first weights are requested before anything else; the scales of the rows (1/32 of the bytes) come next to them, once.
 //
-// The workgroups of the second grid dimension are the tiles of 16 token rows of the experts that have any, found in registers
+// The workgroups are column blocks by tiles of token rows of the experts that have any; a tile is found in registers
 // from the row bounds on the device (a wave holds all of them, four experts per lane): experts without rows cost no workgroup
 // (one token, 8 of 256 experts, H 4096, I 2048: 27 + 17 us; with a workgroup for every expert 39 + 28).
 //
@@ -69,10 +69,12 @@ __global__ __launch_bounds__(256) void expert_stream_mx_kernel(MxArgs a) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
-  // the expert and the rows of tile blockIdx.y
+  // workgroups go through the columns of a tile of token rows, then to the next tile (one dimension: a grid's others end at 65535)
+  const unsigned column_blocks = (unsigned)(a.N / NPER), column = blockIdx.x % column_blocks;
+  // the tile's expert and its rows
   int eg, m0, rb, Me;
   {
-    const int nexp = a.hi - a.lo, want = (int)blockIdx.y;
+    const int nexp = a.hi - a.lo, want = (int)(blockIdx.x / column_blocks);
     int off[5], tiles[4], sum = 0;
 #pragma unroll
     for (int i = 0; i < 5; ++i) off[i] = a.offsets[a.lo + min(lane * 4 + i, nexp)];
@@ -102,13 +104,13 @@ __global__ __launch_bounds__(256) void expert_stream_mx_kernel(MxArgs a) {
   }
   const int rows = min(S::ROWS, Me - m0);
   const int N = a.N, Kdim = a.Kdim, kb32 = Kdim / MX;
-  const int n0 = (int)blockIdx.x * NPER;
+  const int n0 = (int)column * NPER;
   const int nk = (Kdim + 127) / 128;
   const bool half_last = (Kdim & 127) != 0;
   // this wave's part of K: steps [k0, k0 + kn); its walk starts at a step of its own and wraps around (waves that start
   // together would otherwise ask the same memory channels, see expert_stream_lds.hip)
   const int k0 = nk * wave / 4, kn = nk * (wave + 1) / 4 - k0;
-  const int rot = kn > 0 ? (int)((blockIdx.x * 3u + (unsigned)eg * 5u) % (unsigned)kn) : 0;
+  const int rot = kn > 0 ? (int)((column * 3u + (unsigned)eg * 5u) % (unsigned)kn) : 0;
   auto step_of = [&](int s) { return k0 + (s + rot >= kn ? s + rot - kn : s + rot); };
 
   const size_t wrow = (size_t)eg * N + n0;
@@ -313,7 +315,7 @@ int launch_stream_mx_t(const MxArgs& a, hipStream_t st) {
   if (raise_lds_limit((const void*)kern, lds_max, lds_raised) != 0) return -4;
   // tiles of 16 rows: at most one per expert that has rows, and one per 16 rows besides
   const int active = std::min(nexp, a.rows_total), tiles = active + (a.rows_total - active) / S::ROWS;
-  hipLaunchKernelGGL(kern, dim3(a.N / (GATEUP ? S::WROWS / 2 : S::WROWS), tiles), dim3(256), lds, st, a);
+  hipLaunchKernelGGL(kern, dim3((unsigned)(a.N / (GATEUP ? S::WROWS / 2 : S::WROWS)) * (unsigned)tiles), dim3(256), lds, st, a);
   return hipGetLastError() == hipSuccess ? 0 : -4;
 }
 

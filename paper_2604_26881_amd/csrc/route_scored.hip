@@ -23,6 +23,7 @@
 // are 32 * 2^-24 (beyond H 2048 H / 64 * 2^-24) of |x[t]| * max_e |Wr[e]|, which is more than that sum.
 #include "fold.h"
 #include "mx.h"
+#include <algorithm>
 #include <type_traits>
 
 namespace moe {
@@ -121,6 +122,20 @@ __device__ __forceinline__ bool choose(const RouteScored& a, int t, bool want, b
   const bool by_logit = !whole && !a.sigmoid && a.balance == nullptr && (!grouped || a.best == 1);
   auto row_any = [&](bool v) { return ((__ballot(v) >> row0) & ((1ull << LANES) - 1ull)) != 0ull; };
 
+  // Sum over the experts, in an order that does not depend on LANES: rows of 16 lanes add what rows of 32 have in two lanes as
+  // those do, one by one and then the two.
+  constexpr int HALF = LANES == 16 ? EPL / 2 : EPL;
+  auto sum_of = [&](const float (&v)[EPL]) {
+    float part[EPL / HALF];
+#pragma unroll
+    for (int h = 0; h < EPL / HALF; ++h) {
+      part[h] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < HALF; ++i) part[h] += v[HALF * h + i];
+    }
+    return row_sum<LANES>(EPL / HALF == 2 ? part[0] + part[EPL / HALF - 1] : part[0]);
+  };
+
   uint32_t key[EPL];         // what is compared, 0 beyond E
   float m = 0.0f, share = 0.0f;
   double z = 1.0;
@@ -147,10 +162,16 @@ __device__ __forceinline__ bool choose(const RouteScored& a, int t, bool want, b
     }
     if (whole) {             // scores in 64 bits
       if (!a.sigmoid) {
-        double sum = 0.0;
+        double sum = 0.0, part = 0.0;
 #pragma unroll 1
-        for (int i = 0; i < EPL; ++i)
-          if (e0 + i < a.E) sum += exp((double)s_logit[e0 + i] - (double)m);
+        for (int i = 0; i < EPL; ++i) {
+          if (i == HALF) {
+            sum = part;
+            part = 0.0;
+          }
+          if (e0 + i < a.E) part += exp((double)s_logit[e0 + i] - (double)m);
+        }
+        sum += part;
 #pragma unroll
         for (int w = 1; w < LANES; w <<= 1) sum += __shfl_xor(sum, w, WAVE);
         z = sum;
@@ -166,13 +187,9 @@ __device__ __forceinline__ bool choose(const RouteScored& a, int t, bool want, b
 #pragma unroll
       for (int i = 0; i < EPL; ++i) l[i] = __builtin_amdgcn_rcpf(1.0f + __expf(-l[i]));
     } else if (!by_logit) {
-      float sum = 0.0f;
 #pragma unroll
-      for (int i = 0; i < EPL; ++i) {
-        l[i] = e0 + i < a.E ? expf(l[i] - m) : 0.0f;
-        sum += l[i];
-      }
-      sum = row_sum<LANES>(sum);
+      for (int i = 0; i < EPL; ++i) l[i] = e0 + i < a.E ? expf(l[i] - m) : 0.0f;
+      const float sum = sum_of(l);
       z = sum;
       share = 2.1f * doubt + 4e-6f;
       const float inverse = 1.0f / sum;
@@ -400,10 +417,10 @@ __device__ __forceinline__ bool choose(const RouteScored& a, int t, bool want, b
     __builtin_amdgcn_wave_barrier();
   }
   if (by_logit) {            // the weights' denominator
-    float sum = 0.0f;
+    float p[EPL];
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) sum += e0 + i < a.E ? expf(s_logit[e0 + i] - m) : 0.0f;
-    z = row_sum<LANES>(sum);
+    for (int i = 0; i < EPL; ++i) p[i] = e0 + i < a.E ? expf(s_logit[e0 + i] - m) : 0.0f;
+    z = sum_of(p);
   }
   float s = 0.0f;
   if (jl < a.K) {
@@ -595,8 +612,17 @@ int launch_route_scored_t(const RouteScored& a, hipStream_t st) {
   auto kern = route_scored_kernel<NBLK, TT>;
   static std::atomic<uint64_t> lds_raised{0};
   if (raise_lds_limit((const void*)kern, S::LDS, lds_raised) != 0) return -4;
-  hipLaunchKernelGGL(kern, dim3((a.T + S::TOKENS - 1) / S::TOKENS), dim3(64 * ROUTE_WAVES), S::LDS, st, a);
-  return hipGetLastError() == hipSuccess ? 0 : -4;
+  constexpr int most = 1 << 24;          // tokens of a launch (a grid has less than 2^32 threads)
+  for (int t0 = 0; t0 < a.T; t0 += std::min(most, a.T - t0)) {
+    RouteScored part = a;
+    part.x += (size_t)t0 * a.H;
+    part.ids += (size_t)t0 * a.K;
+    part.w += (size_t)t0 * a.K;
+    part.T = std::min(most, a.T - t0);
+    hipLaunchKernelGGL(kern, dim3((part.T + S::TOKENS - 1) / S::TOKENS), dim3(64 * ROUTE_WAVES), S::LDS, st, part);
+    if (hipGetLastError() != hipSuccess) return -4;
+  }
+  return 0;
 }
 
 }  // namespace

@@ -4,6 +4,7 @@
 // holds 8 neighbours (one 16-byte load, one 8-byte store), so the 32 values of a scale are the four lanes of a quad and
 // their maximum is two lane exchanges.
 #include "mx.h"
+#include <algorithm>
 #include <type_traits>
 
 namespace moe {
@@ -41,11 +42,14 @@ __global__ __launch_bounds__(256) void quantize_mx_kernel(const bf16_t* __restri
 
 int launch_quantize_mx(const void* x, int rows, int H, void* q, void* scales, hipStream_t st) {
   const size_t n8 = (size_t)rows * (size_t)(H / 8);
-  const size_t groups = (n8 + 255) / 256;
-  if (groups == 0) return 0;
-  if (groups > 0x7fffffffull) return -2;
-  hipLaunchKernelGGL(quantize_mx_kernel, dim3((unsigned)groups), dim3(256), 0, st, (const bf16_t*)x, n8, (uint8_t*)q, (uint8_t*)scales);
-  return hipGetLastError() == hipSuccess ? 0 : -4;
+  constexpr size_t most = (size_t)1 << 31;      // eighths of a launch (a grid has less than 2^32 threads)
+  for (size_t at = 0; at < n8; at += most) {
+    const size_t n = std::min(most, n8 - at);
+    hipLaunchKernelGGL(quantize_mx_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, (const bf16_t*)x + 8 * at, n,
+                       (uint8_t*)q + 8 * at, (uint8_t*)scales + at / 4);
+    if (hipGetLastError() != hipSuccess) return -4;
+  }
+  return 0;
 }
 
 // Sum of the lanes' values in fp64; every lane returns it
@@ -123,10 +127,16 @@ __global__ __launch_bounds__(256) void residual_norm_mx_kernel(const bf16_t* x, 
 
 int launch_residual_norm_mx(const void* x, const void* y, const void* weight, int T, int H, float eps, void* sum, void* out,
                             void* q, void* scales, hipStream_t st) {
-  if (T == 0) return 0;
-  hipLaunchKernelGGL(residual_norm_mx_kernel, dim3(T), dim3(256), 0, st, (const bf16_t*)x, (const bf16_t*)y, (const bf16_t*)weight, H,
-                     eps, (bf16_t*)sum, (bf16_t*)out, (uint8_t*)q, (uint8_t*)scales);
-  return hipGetLastError() == hipSuccess ? 0 : -4;
+  constexpr int most = 1 << 23;                 // rows of a launch (a grid has less than 2^32 threads)
+  auto from = [](auto* p, size_t n) { return p != nullptr ? p + n : p; };
+  for (int t = 0; t < T; t += std::min(most, T - t)) {
+    const size_t at = (size_t)t * H;
+    hipLaunchKernelGGL(residual_norm_mx_kernel, dim3(std::min(most, T - t)), dim3(256), 0, st, (const bf16_t*)x + at,
+                       from((const bf16_t*)y, at), (const bf16_t*)weight, H, eps, from((bf16_t*)sum, at), from((bf16_t*)out, at),
+                       from((uint8_t*)q, at), from((uint8_t*)scales, at / MX));
+    if (hipGetLastError() != hipSuccess) return -4;
+  }
+  return 0;
 }
 
 }  // namespace moe

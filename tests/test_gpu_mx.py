@@ -442,3 +442,110 @@ def test_batches_of_no_tokens(moe):
     y = moe.moe_expert_group_forward_mx(0, 8, a[2:], torch.zeros(0, dtype=torch.int32, device="cuda"), 2, off, s["Wg"], s["Wu"], s["Wd"], none(s["Yp"]))
     assert y.shape == (0, 128)
     assert moe.moe_quantize_mx(none(s["x"]))[0].shape == (0, 128)
+
+
+# ---- the ends of the ranges
+
+BATCHES = [  # H, E, K, score, groups, top_groups, best, renorm, scale, balance
+    (192, 60, 4, "softmax", 1, 1, 1, False, 1.0, False),
+    (128, 256, 8, "softmax", 8, 3, 2, True, 1.0, True),
+    (128, 176, 6, "softmax", 1, 1, 1, False, 1.0, True),
+    (256, 96, 16, "sigmoid", 16, 4, 2, True, 2.5, True),
+]
+
+
+@pytest.mark.parametrize("case", BATCHES, ids=lambda c: "-".join(map(str, c[:5])))
+def test_route_scored_rows_are_the_same_in_batches_of_every_size(moe, case):
+    H, E, K, score, groups, top, best, renorm, scale, balance = case
+    T = 5003
+    print(f"[case] route_scored batches {case}", flush=True)
+    x, Wr, b = gate_inputs(T, H, E, H + E, (0.1 if score == "sigmoid" else 0.5 / E) if balance else 0.0)
+    x[::7] = x[3]                                              # (and equal rows are equal wherever they stand)
+    run = lambda rows: moe.moe_route_scored(rows.cuda(), Wr.cuda(), None if b is None else b.cuda(), K, score, groups, top, best, renorm, scale)
+    ids, w = run(x)
+    assert torch.equal(w[::7], w[3:4].expand(len(w[::7]), K)) and torch.equal(ids[::7], ids[3:4].expand(len(ids[::7]), K))
+    for lo, hi in ((0, 300), (4990, T), (2500, 2501)):
+        some_ids, some_w = run(x[lo:hi].contiguous())
+        assert torch.equal(some_ids, ids[lo:hi]) and torch.equal(some_w.view(torch.int32), w[lo:hi].view(torch.int32))
+    check_route(moe, x[:40], Wr, b, K, score, groups, top, best, renorm, scale)
+
+
+@pytest.mark.parametrize("T,H,E,K,score,groups,top,best", [(4200, 64, 20, 3, "softmax", 1, 1, 1), (4100, 128, 64, 16, "sigmoid", 16, 5, 2),
+                                                           (33, 128, 256, 16, "sigmoid", 64, 32, 2), (20, 192, 129, 16, "softmax", 43, 6, 1)])
+def test_route_scored_large_batches_and_many_groups(moe, T, H, E, K, score, groups, top, best):
+    print(f"[case] route_scored {T} {H} {E} {K} {score} {groups}", flush=True)
+    x, Wr, b = gate_inputs(T, H, E, T, 0.1 if score == "sigmoid" else 0.5 / E)
+    check_route(moe, x, Wr, b, K, score, groups, top, best, True, 1.0)
+
+
+MORE_COUNTS = [  # mean rows of 13 to 24 (two tiles of 16), above 24, and hundreds; scale rows of odd numbers of pairs and of part groups
+    ([24, 24, 13, 30, 2, 0], 704, 832), ([33, 15, 1, 17, 32, 31, 0, 16], 2048, 1408), ([40, 63, 100, 129, 1, 0, 7], 576, 704),
+    ([40, 63, 100, 129, 1, 0, 7], 640, 576), ([300, 280, 260, 0], 1152, 1216), ([129, 200, 33, 0, 256, 257], 1600, 512), ([26], 4160, 2112),
+]
+
+
+@pytest.mark.parametrize("counts,H,I", MORE_COUNTS, ids=lambda v: str(v).replace(" ", "") if isinstance(v, list) else str(v))
+def test_expert_rows_of_more_sizes(moe, counts, H, I):
+    print(f"[case] experts mx counts={counts} H={H} I={I}", flush=True)
+    c = block_case(moe, counts, H, I, H + I + len(counts))
+    Yp = run_block(moe, c)
+    check_block(c, Yp)
+    # scales of the rows may lie at any even address
+    n = c["x"][1].numel()
+    room = torch.zeros(n + 16, dtype=torch.uint8, device="cuda")
+    for at in (2, 6):
+        room[at:at + n] = c["x"][1].view(torch.uint8).reshape(-1)
+        shifted = room[at:at + n].view(torch.float8_e8m0fnu).view(c["P"], H // 32)
+        assert shifted.data_ptr() % 4 == 2
+        assert torch.equal(bits(run_block(moe, dict(c, x=(c["x"][0], shifted)))), bits(Yp))
+
+
+def test_two_blocks_at_once_share_a_workspace(moe):
+    for counts in ([9, 3, 12, 8, 1, 7], [90, 30, 120, 80, 10, 70]):
+        c = block_case(moe, counts, 512, 640, 6)
+        want = run_block(moe, c)
+        ws = torch.empty(int(moe.load().moe_expert_workspace_bytes(c["P"], c["I"])), dtype=torch.uint8, device="cuda")
+        Yp = torch.zeros_like(want)
+        sides = [torch.cuda.Stream(), torch.cuda.Stream()]
+        torch.cuda.synchronize()
+        for _ in range(3):
+            for stream, (lo, hi) in zip(sides, ((0, 3), (3, 6))):
+                with torch.cuda.stream(stream):
+                    moe.moe_expert_group_forward_mx(lo, hi, c["x"], None, 1, c["off"], c["Wg"], c["Wu"], c["Wd"], Yp, ws)
+        torch.cuda.synchronize()
+        assert torch.equal(bits(Yp), bits(want))
+
+
+def test_more_tiles_than_a_grid_has_in_its_second_dimension(moe):
+    """Short contractions take any number of rows, in tiles of 32."""
+    period, E, H, I = 499, 2, 64, 128
+    counts = [1_300_000, 1_000_001]
+    small = block_case(moe, [period, period], H, I, 12)
+    check_block(small, run_block(moe, small))
+    want = run_block(moe, small)
+    at = torch.cat([torch.arange(n, device="cuda") % period + period * e for e, n in enumerate(counts)])
+    c = dict(small, P=sum(counts), counts=counts, x=tuple(t.view(torch.uint8)[at].view(t.dtype) for t in small["x"]),
+             off=torch.tensor([0, counts[0], sum(counts)], dtype=torch.int32).cuda())
+    assert sum(counts) // 32 > 65535
+    assert torch.equal(bits(run_block(moe, c)), bits(want[at]))
+
+
+def test_rows_beyond_four_gigabytes(moe):
+    period, H, T = 1009, 64, (1 << 23) + 77
+    x = rows(period, H, 8).cuda()
+    y = rows(period, H, 9).cuda()
+    at = torch.arange(T, device="cuda") % period
+    full = moe.moe_residual_norm_mx(x, y)
+    got = moe.moe_residual_norm_mx(x[at], y[at])
+    for a, b in zip(got, full):
+        assert torch.equal(bits(a), bits(b)[at])
+    del got
+    H, T = 16384, 140_003                                      # 4.6 GB of bf16, 2.3 GB of bytes
+    x = rows(7, H, 10).cuda()
+    at = torch.arange(T, device="cuda") % 7
+    q, s = moe.moe_quantize_mx(x)
+    big = x[at]
+    gq, gs = moe.moe_quantize_mx(big)
+    for lo in (0, 65_536, T - 5):
+        assert torch.equal(gq.view(torch.uint8)[lo:lo + 5], q.view(torch.uint8)[at[lo:lo + 5]])
+    assert torch.equal(gs.view(torch.uint8), s.view(torch.uint8)[at])
