@@ -21,8 +21,8 @@
 // 32x32x16 steps; the hidden rows are read in that order of K.  The conversions (32 per wave and step of 1024 MFMA clocks)
 // run beside the other wave's matrix instructions.
 //
-// Rows past the end of an expert repeat its last row and are not stored; 32-row blocks of nothing but such rows are not
-// multiplied.  Weights are copied without a read-once hint: down reads a 128-byte line in two steps, and a hinted line was fetched
+// Rows past the end of an expert repeat its last row and are not stored; 64-row blocks of nothing but such rows are neither
+// copied nor multiplied.  Weights are copied without a read-once hint: down reads a 128-byte line in two steps, and a hinted line was fetched
 // twice (60 experts of 64 rows, H 2048, I 1408: 66 us with it, 55 without).  A row's bits do not depend on the tile height.
 #include <math.h>
 #include <algorithm>
@@ -144,10 +144,15 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
                      l + (uint32_t)wave * 1024u + (uint32_t)(S::TOKENS + (i - S::NLA) * 8192));
     }
   };
-  // copies [FROM, TO) of K step kt (past the end the last step again: the wait counts stay constant) into stage buffer st
-  auto issue = [&](int kt, int st, auto from_, auto to_) {
+  // copies [FROM, TO) of K step kt (past the end the last step again: the wait counts stay constant) into stage buffer st: of the
+  // first TBc * 64 token rows, then of the weights
+  auto issue = [&](auto tbc_, int kt, int st, auto from_, auto to_) {
+    constexpr int TBc = decltype(tbc_)::value;
     const int k = min(kt, nk - 1);
-    for_range<decltype(from_)::value, decltype(to_)::value>([&](auto i_) { issue1(k, st, i_); });
+    for_range<decltype(from_)::value, decltype(to_)::value>([&](auto i_) {
+      constexpr int i = decltype(i_)::value;
+      issue1(k, st, number<(i < TBc ? i : S::NLA + i - TBc)>{});
+    });
   };
   // Scales: 16 bytes of a row are GS steps.  The last group of a row that is not whole groups starts earlier instead, so that it
   // ends with the row.
@@ -201,7 +206,7 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
     t.row0 = __builtin_amdgcn_readlane(vb, owner) + (mrow - __builtin_amdgcn_readlane(vf, owner)) * BM;
     t.rowEnd = __builtin_amdgcn_readlane(ve, owner);
     t.rows = min(BM, t.rowEnd - t.row0);
-    t.tbv = min(S::TB, max(1, (((t.rows + 31) >> 5) - wm + S::WAVES_M - 1) / S::WAVES_M));
+    t.tbv = (t.rows + 63) >> 6;
     t.n0 = nt * S::NOUT;
     if (GATEUP && a.gather != nullptr) {
 #pragma unroll
@@ -240,7 +245,9 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
     }
     for (int s = 0; s < NS; ++s) {
       issue_scales(s);
-      issue(s, s, number<0>{}, number<S::NL>{});
+      for_range<0, S::NL>([&](auto i_) {
+        if (decltype(i_)::value >= S::NLA || decltype(i_)::value < t.tbv) issue1(min(s, nk - 1), s, i_);
+      });
     }
   };
 
@@ -264,19 +271,20 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
     auto pipeline = [&](auto tbc_) {
       constexpr int TBc = decltype(tbc_)::value;
       constexpr int SLOTS = GATEUP ? 2 * TBc : 4;
-      constexpr int PART0 = S::NL - 2 * (S::NL / 3), PART1 = SLOTS > 2 ? PART0 + S::NL / 3 : S::NL;
+      constexpr int NL = TBc + S::NLB;            // copies per wave and stage
+      constexpr int PART0 = NL - 2 * (NL / 3), PART1 = SLOTS > 2 ? PART0 + NL / 3 : NL;
       auto wrow = [&](int nb) { return (GATEUP ? nb * 128 + wn * 32 : wn * 64 + nb * 32) + r32; };
       auto trow = [&](int tb) { return (tb * S::WAVES_M + wm) * 32 + r32; };
       auto slot_copies = [&](auto s_, int kt, int st) {
         constexpr int s = decltype(s_)::value;
         const int before = st == 0 ? NS - 1 : st - 1;
-        if constexpr (s == SLOTS - 1) issue(kt + NS, st, number<0>{}, number<PART0>{});
-        if constexpr (s == 0) issue(kt - 1 + NS, before, number<PART0>{}, number<PART1>{});
-        if constexpr (s == 1 && SLOTS > 2) issue(kt - 1 + NS, before, number<PART1>{}, number<S::NL>{});
+        if constexpr (s == SLOTS - 1) issue(tbc_, kt + NS, st, number<0>{}, number<PART0>{});
+        if constexpr (s == 0) issue(tbc_, kt - 1 + NS, before, number<PART0>{}, number<PART1>{});
+        if constexpr (s == 1 && SLOTS > 2) issue(tbc_, kt - 1 + NS, before, number<PART1>{}, number<NL>{});
       };
       auto publish = [&]() {                      // before a step's last slot
         wait_lds_reads();
-        wait_copies_but<(NS - 2) * S::NL>();      // the next stage has landed
+        wait_copies_but<(NS - 2) * NL>();      // the next stage has landed
         workgroup_barrier();
         __builtin_amdgcn_sched_barrier(0);
       };
@@ -291,7 +299,7 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
         scales = smem + NS * S::STAGE + group_out * S::SCALES;
         scale_at = S::SB * k - group_start(k);
       };
-      wait_copies_but<(NS - 1) * S::NL>();
+      wait_copies_but<(NS - 1) * NL>();
       workgroup_barrier();
       int st = 0;
       if constexpr (GATEUP) {
