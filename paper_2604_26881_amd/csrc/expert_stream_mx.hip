@@ -31,6 +31,7 @@
 // latencies: row bounds, sort, first lines, two more, the sum, the store.
 //
 // A last step of 64 (contractions that are not whole steps) copies its bytes twice and multiplies zeros in the second half.
+#include "fold.h"
 #include "mx.h"
 #include <algorithm>
 #include <type_traits>
@@ -49,17 +50,6 @@ struct StreamMxShape {
   static constexpr int LDP = ROWS + 1;                      // partial sums: [WROWS][LDP], a padding word per row
   static_assert(STAGE >= WROWS * LDP * 4, "a wave's partial sums take the place of its stage");
 };
-
-// Inclusive sum over the lanes of a wave
-__device__ __forceinline__ int wave_scan(int v) {
-  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);      // within rows of 16: from 1, 2, 4, 8 lanes before
-  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);      // a row's last lane to the next row
-  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);      // lane 31 to the upper half
-  return v;
-}
 
 template <int MT, int WB, bool GATEUP>
 __global__ __launch_bounds__(256) void expert_stream_mx_kernel(MxArgs a) {

@@ -6,11 +6,15 @@
 // A tile is BM token rows of one expert by 256 weight rows (gate/up: 128 gate rows and the matching 128 up rows), eight waves
 // as 2 x 4, each on BM / 2 token rows by 64 weight rows (a gate block of 32 and its up block).  The kernel is persistent: every
 // wave forms the tiles of the experts in registers from the row bounds on the device and walks tile numbers with a fixed
-// stride, as the bf16 tile kernels do (expert_tile.hip has the measurements behind that walk: XCDs take runs of neighbouring
-// tiles, experts with few and with many tiles are drawn in turn).
+// stride; XCDs take runs of neighbouring tiles.  The numbers go from the highest tiles to the lowest, so every workgroup gets
+// as many of each height as the others but for one, and every other XCD walks backwards, so that high tiles (bound by the
+// matrix cores) and low ones (by the weights' bytes) run side by side.  With the experts in order and those of few rows strewn
+// in, some workgroups had half again as much as others: 4096 tokens drawn by rank (E 60, H 2048, I 1408) 173 + 152 us, this
+// way 162 + 137; 2000 such tokens (E 128, H 1024, I 768) 66 + 72, 60 + 60.  With many rows everywhere the order by expert was
+// the better one, by the weights that an expert's last tile shares with its others: 16 384 tokens 440 + 380, 463 + 381.
 //
-// K steps of 128 (gate/up) or 64 (down: a bf16 row has as many bytes) through a ring of NS LDS stages filled by asynchronous
-// copies, a row's 16-byte chunks xor-swizzled against bank conflicts; one barrier per step.  Scales come 16 bytes of a row at a
+// K steps of 128 (gate/up) or 64 (down: a bf16 row has as many bytes) through a ring of LDS stages filled by asynchronous
+// copies, more of them the lower the tile, a row's 16-byte chunks xor-swizzled against bank conflicts; one barrier per step.  Scales come 16 bytes of a row at a
 // time, those of 4 (gate/up) or 8 steps, into two buffers of their own: every row is another cache line, and fetched step by step
 // they cost as many line requests as the rows themselves (one expert of 16 384 rows, H 8192, I 4096, gate/up: 1004 us, this way 916,
 // without any scales 872).
@@ -27,6 +31,7 @@
 #include <math.h>
 #include <algorithm>
 #include <type_traits>
+#include "fold.h"
 #include "mx.h"
 
 namespace moe {
@@ -34,7 +39,7 @@ namespace {
 
 constexpr int TILE_MX_EMAX = 256;
 
-template <int BM, bool GATEUP, int NS, bool TAIL>
+template <int BM, bool GATEUP, bool TAIL>
 struct TileMxShape {
   static constexpr int BN = 256, WAVES_M = 2, WAVES_N = 4, NW = 8;
   static constexpr int TB = BM / 64, NB = 2;                // 32-row blocks of a wave: tokens, weights
@@ -42,17 +47,23 @@ struct TileMxShape {
   static constexpr int BK = GATEUP ? 128 : 64;              // K values per step
   static constexpr int WROWB = GATEUP ? 128 : 64;           // bytes per staged weight row (token rows: 128)
   static constexpr int SROWS = GATEUP ? BM + BN : BN;       // rows with scales
-  static constexpr int TOKENS = BM * 128, WEIGHTS = BN * WROWB;
-  static constexpr int STAGE = TOKENS + WEIGHTS;
   static constexpr int SB = GATEUP ? 4 : 2, GS = 16 / SB;   // scale bytes per row and step, steps per group of 16 bytes
-  static constexpr int SCALES = SROWS * 16, LDS = NS * STAGE + 2 * SCALES + 16;    // (a last row's pair of dwords ends behind it)
-  static constexpr int NLA = BM / 64;                       // 1 KB copies per wave and stage: token rows,
-  static constexpr int NLB = GATEUP ? 4 : 2;                // weight rows (and, once per group, scales of 64 rows)
-  static constexpr int NL = NLA + NLB;
+  static constexpr int SCALES = SROWS * 16;                 // a group; two of them lie in front of the stages
+  // copies of 1 KB per wave and stage: 64 token rows each, weight rows (and, once per group, scales of 64 rows)
+  static constexpr int NLA = TB, NLB = GATEUP ? 4 : 2;
+  // for a tile of 64 h rows: bytes of a stage's tokens and of a stage, and how many stages fit
+  static constexpr int tokens(int h) { return h * 8192; }
+  static constexpr int stage(int h) { return tokens(h) + BN * WROWB; }
+  static constexpr int ring(int h) { return std::min(GS, (160 * 1024 - 2 * SCALES) / stage(h)); }
+  static constexpr int lds() {
+    int most = 0;
+    for (int h = 1; h <= TB; ++h) most = std::max(most, ring(h) * stage(h));
+    return 2 * SCALES + most;
+  }
   static constexpr int GM = 4;                              // token tiles per locality group of the walk
   static_assert(GATEUP || !TAIL, "the down projection's steps are half as long");
-  static_assert(NS >= 2 && NS * NL < 60 && NS <= GS && LDS <= 160 * 1024 && SROWS / 64 <= NW,
-                "wait counter; two groups of scales in LDS are enough; LDS; a copy of scales per wave");
+  static_assert(ring(TB) >= 2 && ring(1) * (1 + NLB) < 60 && ring(TB) * (TB + NLB) < 60 && SROWS / 64 <= NW,
+                "two stages at least, the wait counter, a copy of scales per wave");
 };
 constexpr int TILE_MX_MIN_K = 512;       // a row has 16 scale bytes
 
@@ -66,56 +77,48 @@ __device__ __forceinline__ void for_range(F&& f) {
   }
 }
 
-template <int BM, bool GATEUP, int NS, bool TAIL>
+template <int BM, bool GATEUP, bool TAIL>
 __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
-  using S = TileMxShape<BM, GATEUP, NS, TAIL>;
+  using S = TileMxShape<BM, GATEUP, TAIL>;
   extern __shared__ __align__(16) unsigned char smem[];
-  constexpr int HEAVY_MIN = 3;       // token tiles from which an expert counts as bound by the matrix cores
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / S::WAVES_N, wn = wave % S::WAVES_N;
   const int nexp = a.hi - a.lo;
 
-  // rows [rb, re) and tiles [first, last) (in its class's list) of four experts per lane
-  int first[4], last[4], rb[4], re[4], cnt[2] = {0, 0};
+  // Tiles by their height in blocks of 64 rows, 1 .. TB: of every expert the whole ones, and what is left over.  Four experts per
+  // lane: rows [rb, re), the place of the first whole tile among those of height TB, of the rest among those of its height.
+  int rb[4], re[4], whole[4], rest[4], total[S::TB];
+  auto whole_tiles = [&](int i) { return (re[i] - rb[i]) / BM; };
+  auto rest_height = [&](int i) { return ((re[i] - rb[i]) % BM + 63) >> 6; };
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int e = lane * 4 + i;
     rb[i] = e < nexp ? a.offsets[a.lo + e] : 0;
-    re[i] = e < nexp ? a.offsets[a.lo + e + 1] : 0;
-    last[i] = (max(re[i] - rb[i], 0) + BM - 1) / BM;
-    cnt[last[i] >= HEAVY_MIN] += last[i];
+    re[i] = max(rb[i], e < nexp ? a.offsets[a.lo + e + 1] : 0);
+    whole[i] = rest[i] = 0;
   }
-  int total[2];
 #pragma unroll
-  for (int c = 0; c < 2; ++c) {
-    int incl = cnt[c];
+  for (int h = 1; h <= S::TB; ++h) {
+    int n[4], sum = 0;
 #pragma unroll
-    for (int s = 1; s < 64; s <<= 1) {
-      const int o = __shfl_up(incl, s, WAVE);
-      if (lane >= s) incl += o;
+    for (int i = 0; i < 4; ++i) sum += n[i] = (h == S::TB ? whole_tiles(i) : 0) + (rest_height(i) == h ? 1 : 0);
+    const int upto = wave_scan(sum);
+    total[h - 1] = __builtin_amdgcn_readlane(upto, 63);
+    int at = upto - sum;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (h == S::TB) whole[i] = at;
+      else rest[i] = rest_height(i) == h ? at : rest[i];
+      at += n[i];
     }
-    total[c] = __builtin_amdgcn_readlane(incl, 63);
-    cnt[c] = incl - cnt[c];
   }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const bool heavy = last[i] >= HEAVY_MIN;
-    first[i] = heavy ? cnt[1] : cnt[0];
-    last[i] += first[i];
-    cnt[0] = heavy ? cnt[0] : last[i];
-    cnt[1] = heavy ? last[i] : cnt[1];
-  }
-  const int total0 = total[0], total1 = total[1];
-  const int grp0 = (total0 + S::GM - 1) / S::GM, grp1 = (total1 + S::GM - 1) / S::GM;   // locality groups per class
-  const int ngrp = grp0 + grp1;
   const int N = a.N, Kdim = a.Kdim, kb32 = Kdim / MX;
   const int NT = (N + S::NOUT - 1) / S::NOUT;
   const int nk = (Kdim + S::BK - 1) / S::BK;
-  const int groupTiles = S::GM * NT;
-  const int Lend = grp0 == 0 || grp1 == 0 ? (total0 + total1) * NT : ngrp * groupTiles;
-  // light groups among the first g of the merged walk: (g * light_ratio) >> 32, exactly grp0 at g = ngrp
-  const unsigned long long light_ratio = ngrp > 0 ? ((((unsigned long long)grp0) << 32) + (unsigned)ngrp - 1ull) / (unsigned)ngrp : 0ull;
+  int Lend = 0;
+#pragma unroll
+  for (int h = 0; h < S::TB; ++h) Lend += total[h] * NT;
 
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
   const int crow = lane >> 3, cchunk = (lane & 7) ^ crow;   // copies of 128-byte rows: row lane/8, slot lane%8 holding chunk slot xor row%8
@@ -128,32 +131,26 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
   const int slot = xcd_walk ? (int)(blockIdx.x >> 3) : 0;
   const int run = xcd_walk ? max(1, min(G >> 3, (Lend + 7) >> 3)) : 1;
   if (xcd_walk && slot >= run) return;
+  const int L0 = xcd_walk ? (int)(blockIdx.x & 7) * run + slot : (int)blockIdx.x, step = xcd_walk ? 8 * run : G;
+  const int its = L0 < Lend ? (Lend - L0 + step - 1) / step : 0;
+  const bool back = xcd_walk && (blockIdx.x & 1) != 0;      // half of the XCDs begin with the low tiles
 
   struct Tile { int row0, rowEnd, eg, rows, tbv, n0; bool valid; };
   const uint8_t *Ag = nullptr, *Bg0 = nullptr, *Bg1 = nullptr, *Sg = nullptr;
   uint32_t coff[S::NLA + S::NLB], soff = 0;     // byte offsets of this lane's parts of a stage's copies, at K step 0
-  // copy i of a stage: token rows, weight rows, scales
-  auto issue1 = [&](int k, int st, auto i_) {
-    constexpr int i = decltype(i_)::value;
-    const uint32_t l = lds0 + (uint32_t)st * S::STAGE;
-    const uint32_t back = TAIL && k == nk - 1 ? tail_back : 0u;     // the missing half from the half that is there
-    if constexpr (i < S::NLA) {
-      copy_to_lds_16(Ag + (size_t)k * 128, coff[i] - back, l + (uint32_t)wave * 1024u + (uint32_t)i * 8192u);
-    } else {
-      copy_to_lds_16((GATEUP && i >= S::NLA + 2 ? Bg1 : Bg0) + (size_t)k * S::WROWB, coff[i] - back,
-                     l + (uint32_t)wave * 1024u + (uint32_t)(S::TOKENS + (i - S::NLA) * 8192));
-    }
-  };
-  // copies [FROM, TO) of K step kt (past the end the last step again: the wait counts stay constant) into stage buffer st: of the
-  // first TBc * 64 token rows, then of the weights
-  auto issue = [&](auto tbc_, int kt, int st, auto from_, auto to_) {
+  // copies [FROM, TO) of K step k into stage buffer st of a tile of TBc * 64 rows: its token rows, then the weights
+  auto issue_step = [&](auto tbc_, int k, int st, auto from_, auto to_) {
     constexpr int TBc = decltype(tbc_)::value;
-    const int k = min(kt, nk - 1);
+    const uint32_t l = lds0 + (uint32_t)(2 * S::SCALES + wave * 1024) + (uint32_t)st * S::stage(TBc);
+    const uint32_t back = TAIL && k == nk - 1 ? tail_back : 0u;     // the missing half from the half that is there
     for_range<decltype(from_)::value, decltype(to_)::value>([&](auto i_) {
-      constexpr int i = decltype(i_)::value;
-      issue1(k, st, number<(i < TBc ? i : S::NLA + i - TBc)>{});
+      constexpr int i = decltype(i_)::value, w = i - TBc;
+      if constexpr (w < 0) copy_to_lds_16(Ag + (size_t)k * 128, coff[i] - back, l + (uint32_t)i * 8192u);
+      else copy_to_lds_16((GATEUP && w >= 2 ? Bg1 : Bg0) + (size_t)k * S::WROWB, coff[S::NLA + w] - back, l + (uint32_t)(S::tokens(TBc) + w * 8192));
     });
   };
+  // of K step kt; past the end the last step again: the wait counts stay constant
+  auto issue = [&](auto tbc_, int kt, int st, auto from_, auto to_) { issue_step(tbc_, min(kt, nk - 1), st, from_, to_); };
   // Scales: 16 bytes of a row are GS steps.  The last group of a row that is not whole groups starts earlier instead, so that it
   // ends with the row.
   auto group_start = [&](int k) { return min(k / S::GS * 16, kb32 - 16); };
@@ -164,7 +161,7 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
     const int k = min(kt, nk - 1);
     if (k % S::GS == 0 && kt < nk) {
       if (wave < S::SROWS / 64)
-        copy_to_lds_16(Sg + group_start(k), soff, lds0 + (uint32_t)(NS * S::STAGE + group_in * S::SCALES) + (uint32_t)wave * 1024u);
+        copy_to_lds_16(Sg + group_start(k), soff, lds0 + (uint32_t)(group_in * S::SCALES) + (uint32_t)wave * 1024u);
       group_in ^= 1;
     }
   };
@@ -175,36 +172,36 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
   int gathered[S::NLA + 1];
   auto find_tile = [&]() -> Tile {
     Tile t{};
-    int mrow = 0, nt = 0, cls = 0;
-    for (;; ++it) {
-      const int L = xcd_walk ? ((it * 8 + (int)(blockIdx.x & 7)) * run + slot) : (it * G + (int)blockIdx.x);
-      if (L >= Lend) return t;
-      const int grp = L / groupTiles, rem = L - grp * groupTiles;
-      const int before = (int)(((unsigned long long)(unsigned)grp * light_ratio) >> 32);
-      cls = (int)(((unsigned long long)(unsigned)(grp + 1) * light_ratio) >> 32) > before ? 0 : 1;
-      const int g0 = (cls == 0 ? before : grp - before) * S::GM;
-      const int size = min(S::GM, (cls == 0 ? total0 : total1) - g0);
-      nt = rem / size;
-      mrow = g0 + rem - nt * size;
-      if (nt < NT) break;
-    }
+    if (it >= its) return t;
+    int at = L0 + (back ? its - 1 - it : it) * step, h = S::TB;
     ++it;
+    int tiles = total[S::TB - 1];
+#pragma unroll
+    for (int i = S::TB - 1; i >= 1; --i)
+      if (h == i + 1 && at >= tiles * NT) {
+        at -= tiles * NT;
+        h = i;
+        tiles = total[i - 1];
+      }
+    // groups of GM tiles of token rows go through the columns together
+    const int g0 = at / (S::GM * NT) * S::GM, size = min(S::GM, tiles - g0);
+    const int rem = at - g0 * NT, nt = rem / size, mrow = g0 + rem - nt * size;
     t.valid = true;
-    int at = 0, vf = 0, vb = 0, ve = 0;
+    int slot_of = 0, r0 = 0, r1 = 0;
     unsigned long long found = 0ull;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const bool mine = (last[i] - first[i] >= HEAVY_MIN) == (cls == 1) && first[i] <= mrow && mrow < last[i];
+      const int n = whole_tiles(i), low = rest_height(i);
+      const bool mine = h == S::TB ? mrow >= whole[i] && mrow < whole[i] + n + (low == S::TB ? 1 : 0) : low == h && mrow == rest[i];
       found |= __ballot(mine);
-      at = mine ? i : at;
-      vf = mine ? first[i] : vf;
-      vb = mine ? rb[i] : vb;
-      ve = mine ? re[i] : ve;
+      slot_of = mine ? i : slot_of;
+      r0 = mine ? rb[i] + (h == S::TB ? mrow - whole[i] : n) * BM : r0;
+      r1 = mine ? re[i] : r1;
     }
     const int owner = __builtin_ctzll(found);
-    t.eg = a.lo + owner * 4 + __builtin_amdgcn_readlane(at, owner);
-    t.row0 = __builtin_amdgcn_readlane(vb, owner) + (mrow - __builtin_amdgcn_readlane(vf, owner)) * BM;
-    t.rowEnd = __builtin_amdgcn_readlane(ve, owner);
+    t.eg = a.lo + owner * 4 + __builtin_amdgcn_readlane(slot_of, owner);
+    t.row0 = __builtin_amdgcn_readlane(r0, owner);
+    t.rowEnd = __builtin_amdgcn_readlane(r1, owner);
     t.rows = min(BM, t.rowEnd - t.row0);
     t.tbv = (t.rows + 63) >> 6;
     t.n0 = nt * S::NOUT;
@@ -243,12 +240,15 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
       Sg = (GATEUP && w >= 2 ? a.B1s : a.B0s) + wrow * kb32;
       soff = (uint32_t)column((GATEUP ? w & 1 : w) * 64 + lane) * (uint32_t)kb32;
     }
-    for (int s = 0; s < NS; ++s) {
-      issue_scales(s);
-      for_range<0, S::NL>([&](auto i_) {
-        if (decltype(i_)::value >= S::NLA || decltype(i_)::value < t.tbv) issue1(min(s, nk - 1), s, i_);
-      });
-    }
+    for_range<1, S::TB + 1>([&](auto h_) {
+      constexpr int h = decltype(h_)::value;
+      if (t.tbv == h) {
+        for (int st = 0; st < S::ring(h); ++st) {
+          issue_scales(st);
+          issue(h_, st, st, number<0>{}, number<h + S::NLB>{});
+        }
+      }
+    });
   };
 
   Tile cur = find_tile();
@@ -263,7 +263,7 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[nb][tb][i] = 0.0f;
 
-    // Software pipeline.  All NS stages of the tile have been requested (next_tile).  A step is cut into slots of matrix
+    // Software pipeline.  All NS stages of the tile have been requested (request_tile).  A step is cut into slots of matrix
     // instructions; a slot's operands are read from LDS during the slot before, those of a step's first slot during the last slot of
     // the step before, behind the barrier that publishes the step's stage.  That barrier also says that everybody has the step
     // before it in registers, so its buffer takes the copies of the stage NS steps ahead: a part in that slot, the rest in the
@@ -271,7 +271,8 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
     auto pipeline = [&](auto tbc_) {
       constexpr int TBc = decltype(tbc_)::value;
       constexpr int SLOTS = GATEUP ? 2 * TBc : 4;
-      constexpr int NL = TBc + S::NLB;            // copies per wave and stage
+      constexpr int NS = S::ring(TBc), STAGE = S::stage(TBc), TOKENS = S::tokens(TBc), NL = TBc + S::NLB;      // (NL: copies per wave and stage)
+      const unsigned char* const stages = smem + 2 * S::SCALES;
       constexpr int PART0 = NL - 2 * (NL / 3), PART1 = SLOTS > 2 ? PART0 + NL / 3 : NL;
       auto wrow = [&](int nb) { return (GATEUP ? nb * 128 + wn * 32 : wn * 64 + nb * 32) + r32; };
       auto trow = [&](int tb) { return (tb * S::WAVES_M + wm) * 32 + r32; };
@@ -290,13 +291,13 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
       };
       // at the top of a step: the scales of the stage requested next, and where those of the next step (byte `scale_at` of each
       // row's 16, in LDS at `scales`) will be
-      const unsigned char* scales = smem + NS * S::STAGE + group_out * S::SCALES;
+      const unsigned char* scales = smem + group_out * S::SCALES;
       int scale_at = -group_start(0);
       auto scales_top = [&](int kt) {
         issue_scales(kt + NS);
         const int k = min(kt + 1, nk - 1);
         if (kt + 1 < nk && k % S::GS == 0) group_out ^= 1;
-        scales = smem + NS * S::STAGE + group_out * S::SCALES;
+        scales = smem + group_out * S::SCALES;
         scale_at = S::SB * k - group_start(k);
       };
       wait_copies_but<(NS - 1) * NL>();
@@ -312,7 +313,7 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
         };
         auto read_w = [&](const unsigned char* base, auto m_) {
 #pragma unroll
-          for (int nb = 0; nb < S::NB; ++nb) read_row(w[decltype(m_)::value][nb], base + S::TOKENS + wrow(nb) * 128, m_);
+          for (int nb = 0; nb < S::NB; ++nb) read_row(w[decltype(m_)::value][nb], base + TOKENS + wrow(nb) * 128, m_);
         };
         auto read_x = [&](const unsigned char* base, auto s_) {
           constexpr int s = decltype(s_)::value;
@@ -333,10 +334,10 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
           for (int tb = 0; tb < TBc; ++tb) sx[tb] = one(trow(tb));
         };
         read_scales();
-        read_w(smem, number<0>{});
-        read_x(smem, number<0>{});
+        read_w(stages, number<0>{});
+        read_x(stages, number<0>{});
         for (int kt = 0; kt < nk; ++kt) {
-          const unsigned char* base = smem + st * S::STAGE;
+          const unsigned char* base = stages + st * STAGE;
           const int st1 = st + 1 == NS ? 0 : st + 1;
           scales_top(kt);
           const uint32_t there = !TAIL || kt != nk - 1 ? ~0u : 0u;      // a step's second half
@@ -363,7 +364,7 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
               read_x(base, number<s + 1>{});
               if constexpr (s == (TBc > 1 ? TBc - 2 : 0)) read_w(base, number<1>{});
             } else {
-              const unsigned char* next = smem + st1 * S::STAGE;
+              const unsigned char* next = stages + st1 * STAGE;
               read_x(next, number<0>{});
               read_w(next, number<0>{});
               read_scales();
@@ -383,7 +384,7 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
           constexpr int p = decltype(p_)::value;
 #pragma unroll
           for (int nb = 0; nb < S::NB; ++nb)
-            raw[p][nb] = *reinterpret_cast<const u32x4*>(base + S::TOKENS + wrow(nb) * 64 + (((2 * p + half) ^ ((lane >> 2) & 3)) << 4));
+            raw[p][nb] = *reinterpret_cast<const u32x4*>(base + TOKENS + wrow(nb) * 64 + (((2 * p + half) ^ ((lane >> 2) & 3)) << 4));
         };
         auto read_scales = [&]() {
 #pragma unroll
@@ -399,18 +400,18 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
           for (int nb = 0; nb < S::NB; ++nb) wf[j][nb] = mx_to_bf16(raw[p][nb][2 * j], raw[p][nb][2 * j + 1], (int)((sw[nb] >> (8 * p)) & 255u));
         };
         read_scales();
-        read_raw(smem, number<0>{});
+        read_raw(stages, number<0>{});
 #pragma unroll
-        for (int tb = 0; tb < TBc; ++tb) read_x1(smem, number<0>{}, tb);
+        for (int tb = 0; tb < TBc; ++tb) read_x1(stages, number<0>{}, tb);
         convert(number<0>{});
         for (int kt = 0; kt < nk; ++kt) {
-          const unsigned char* base = smem + st * S::STAGE;
+          const unsigned char* base = stages + st * STAGE;
           const int st1 = st + 1 == NS ? 0 : st + 1;
           scales_top(kt);
           for_range<0, SLOTS>([&](auto s_) {
             constexpr int s = decltype(s_)::value;
             if constexpr (s == SLOTS - 1) publish();
-            const unsigned char* from = s < SLOTS - 1 ? base : smem + st1 * S::STAGE;
+            const unsigned char* from = s < SLOTS - 1 ? base : stages + st1 * STAGE;
             constexpr int NM = S::NB * TBc;       // matrix instructions of the slot: behind the first ones the reads, then the copies
 #pragma unroll
             for (int j = 0; j < NM; ++j) {
@@ -485,11 +486,11 @@ int num_cus() {
   return n;
 }
 
-template <int BM, bool GATEUP, int NS, bool TAIL>
+template <int BM, bool GATEUP, bool TAIL>
 int launch_tile_mx_t(const MxArgs& a, hipStream_t st) {
-  using S = TileMxShape<BM, GATEUP, NS, TAIL>;
-  auto kern = expert_tile_mx_kernel<BM, GATEUP, NS, TAIL>;
-  constexpr int lds = S::LDS;
+  using S = TileMxShape<BM, GATEUP, TAIL>;
+  auto kern = expert_tile_mx_kernel<BM, GATEUP, TAIL>;
+  constexpr int lds = S::lds();
   if (a.Kdim < TILE_MX_MIN_K) return -2;
   static std::atomic<uint64_t> lds_raised{0};
   const int nexp = a.hi - a.lo;
@@ -511,10 +512,10 @@ int launch_tile_mx_t(const MxArgs& a, hipStream_t st) {
 int launch_tile_mx_gateup(const MxArgs& a, hipStream_t st) {
   const bool half_last = a.Kdim % 128 != 0;
   if (a.mean_rows + 1.5 * sqrt((double)a.mean_rows) <= 128.0)
-    return half_last ? launch_tile_mx_t<128, true, 3, true>(a, st) : launch_tile_mx_t<128, true, 3, false>(a, st);
-  return half_last ? launch_tile_mx_t<256, true, 2, true>(a, st) : launch_tile_mx_t<256, true, 2, false>(a, st);
+    return half_last ? launch_tile_mx_t<128, true, true>(a, st) : launch_tile_mx_t<128, true, false>(a, st);
+  return half_last ? launch_tile_mx_t<256, true, true>(a, st) : launch_tile_mx_t<256, true, false>(a, st);
 }
 // Down: 256 rows always.  (The same experts, of 48 rows 49 us and 52 in tiles of 128, of 100 rows 64 and 63, of 150 rows 71 and 99.)
-int launch_tile_mx_down(const MxArgs& a, hipStream_t st) { return launch_tile_mx_t<256, false, 3, false>(a, st); }
+int launch_tile_mx_down(const MxArgs& a, hipStream_t st) { return launch_tile_mx_t<256, false, false>(a, st); }
 
 }  // namespace moe
