@@ -3,21 +3,25 @@
 //   gate/up : h[r, n]  = bf16( silu(<A[r,:], Wg[e][n,:]>) * <A[r,:], Wu[e][n,:]> )     rows and weights in 8 bits
 //   down    : Yp[r, n] = bf16( <h[r,:], Wd[e][n,:]> )                                  bf16 rows, 8-bit weights
 //
-// A tile is BM token rows of one expert by 256 weight rows (gate/up: 128 gate rows and the matching 128 up rows), eight waves
-// as 2 x 4, each on BM / 2 token rows by 64 weight rows (a gate block of 32 and its up block).  The kernel is persistent: every
-// wave forms the tiles of the experts in registers from the row bounds on the device and walks tile numbers with a fixed
-// stride; XCDs take runs of neighbouring tiles.  The numbers go from the highest tiles to the lowest, so every workgroup gets
-// as many of each height as the others but for one, and every other XCD walks backwards, so that high tiles (bound by the
-// matrix cores) and low ones (by the weights' bytes) run side by side.  With the experts in order and those of few rows strewn
-// in, some workgroups had half again as much as others: 4096 tokens drawn by rank (E 60, H 2048, I 1408) 173 + 152 us, this
-// way 162 + 137; 2000 such tokens (E 128, H 1024, I 768) 66 + 72, 60 + 60.  With many rows everywhere the order by expert was
-// the better one, by the weights that an expert's last tile shares with its others: 16 384 tokens 440 + 380, 463 + 381.
+// A tile is up to 256 token rows of one expert by 256 weight rows (gate/up: 128 gate rows and the matching 128 up rows), eight
+// waves as 2 x 4, each on half of the token rows by 64 weight rows (a gate block of 32 and its up block).  Its height is whole
+// blocks of 64 rows.  (Tiles of at most 128 rows, with as many stages, were up to 4 % faster for experts of 50 to 200 rows, and
+// far slower for more.)
+//
+// The kernel is persistent: every wave forms the tiles of the experts in registers from the row bounds on the device and walks
+// tile numbers with a fixed stride; XCDs take runs of neighbouring tiles.  The numbers go from the highest tiles to the lowest,
+// so every workgroup gets as many of each height as the others but for one, and every other XCD walks backwards, so that high
+// tiles (bound by the matrix cores) and low ones (by the weights' bytes) run side by side.  With the experts in order and those
+// of few rows strewn in, some workgroups had half again as much as others: 4096 tokens drawn by rank (E 60, H 2048, I 1408)
+// 173 + 152 us, this way 162 + 137; 2000 such tokens (E 128, H 1024, I 768) 66 + 72, 60 + 60.  With many rows everywhere the
+// order by expert was the better one, by the weights that an expert's last tile shares with its others: 16 384 tokens
+// 440 + 380 us, 463 + 381.
 //
 // K steps of 128 (gate/up) or 64 (down: a bf16 row has as many bytes) through a ring of LDS stages filled by asynchronous
-// copies, more of them the lower the tile, a row's 16-byte chunks xor-swizzled against bank conflicts; one barrier per step.  Scales come 16 bytes of a row at a
-// time, those of 4 (gate/up) or 8 steps, into two buffers of their own: every row is another cache line, and fetched step by step
-// they cost as many line requests as the rows themselves (one expert of 16 384 rows, H 8192, I 4096, gate/up: 1004 us, this way 916,
-// without any scales 872).
+// copies, more of them the lower the tile, a row's 16-byte chunks xor-swizzled against bank conflicts; one barrier per step.
+// Scales come 16 bytes of a row at a time, those of 4 (gate/up) or 8 steps, into two buffers of their own: every row is another
+// cache line, and fetched step by step they cost as many line requests as the rows themselves (one expert of 16 384 rows,
+// H 8192, I 4096, gate/up: 1004 us, this way 916, without any scales 872).
 //
 // Gate/up multiplies with 32x32x64 on 8-bit values: a lane holds of row lane % 32 the chunks 4m + h and 4m + 2 + h of the
 // step's half m (h = lane / 32) and gives the scale of block 2m + h: the row's slot, shifted by h bytes, and a byte select.
@@ -26,9 +30,15 @@
 // run beside the other wave's matrix instructions.
 //
 // Rows past the end of an expert repeat its last row and are not stored; 64-row blocks of nothing but such rows are neither
-// copied nor multiplied.  Weights are copied without a read-once hint: down reads a 128-byte line in two steps, and a hinted line was fetched
-// twice (60 experts of 64 rows, H 2048, I 1408: 66 us with it, 55 without).  A row's bits do not depend on the tile height.
-#include <math.h>
+// copied nor multiplied.  Weights are copied without a read-once hint: down reads a 128-byte line in two steps, and a hinted
+// line was fetched twice (60 experts of 64 rows, H 2048, I 1408: 66 us with it, 55 without).  A row's bits do not depend on the
+// tile's height.
+//
+// Measured: one expert of 16 384 rows, H 8192, I 4096: gate/up 895 us, 2.46 PFLOP/s, down 805, 1.37.  16 384 tokens on 60
+// experts, H 2048, I 1408: 463 + 381 us; what is lost against the former's rates are the first and last steps of tiles of 16
+// and 22 steps, the sigmoid and the stores (65 us of gate/up), and 5 % to workgroups that wait for the last ones.  Gate/up runs
+// at 1.8 GHz, the card's power limit, so fewer waits alone make it no faster: another barrier per step that let copies start
+// half a step earlier changed nothing.
 #include <algorithm>
 #include <type_traits>
 #include "fold.h"
@@ -39,9 +49,9 @@ namespace {
 
 constexpr int TILE_MX_EMAX = 256;
 
-template <int BM, bool GATEUP, bool TAIL>
+template <bool GATEUP, bool TAIL>
 struct TileMxShape {
-  static constexpr int BN = 256, WAVES_M = 2, WAVES_N = 4, NW = 8;
+  static constexpr int BM = 256, BN = 256, WAVES_M = 2, WAVES_N = 4, NW = 8;
   static constexpr int TB = BM / 64, NB = 2;                // 32-row blocks of a wave: tokens, weights
   static constexpr int NOUT = GATEUP ? BN / 2 : BN;         // output columns of a tile
   static constexpr int BK = GATEUP ? 128 : 64;              // K values per step
@@ -77,9 +87,10 @@ __device__ __forceinline__ void for_range(F&& f) {
   }
 }
 
-template <int BM, bool GATEUP, bool TAIL>
+template <bool GATEUP, bool TAIL>
 __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
-  using S = TileMxShape<BM, GATEUP, TAIL>;
+  using S = TileMxShape<GATEUP, TAIL>;
+  constexpr int BM = S::BM;
   extern __shared__ __align__(16) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -486,10 +497,10 @@ int num_cus() {
   return n;
 }
 
-template <int BM, bool GATEUP, bool TAIL>
+template <bool GATEUP, bool TAIL>
 int launch_tile_mx_t(const MxArgs& a, hipStream_t st) {
-  using S = TileMxShape<BM, GATEUP, TAIL>;
-  auto kern = expert_tile_mx_kernel<BM, GATEUP, TAIL>;
+  using S = TileMxShape<GATEUP, TAIL>;
+  auto kern = expert_tile_mx_kernel<GATEUP, TAIL>;
   constexpr int lds = S::lds();
   if (a.Kdim < TILE_MX_MIN_K) return -2;
   static std::atomic<uint64_t> lds_raised{0};
@@ -497,7 +508,7 @@ int launch_tile_mx_t(const MxArgs& a, hipStream_t st) {
   if (nexp > TILE_MX_EMAX) return -2;
   if (raise_lds_limit((const void*)kern, lds, lds_raised) != 0) return -4;
   const long NT = (a.N + S::NOUT - 1) / S::NOUT;
-  const long bound = (((long)a.rows_total / BM + nexp + S::GM - 1) / S::GM) * S::GM * NT;
+  const long bound = (((long)a.rows_total / S::BM + nexp + S::GM - 1) / S::GM) * S::GM * NT;
   const int grid = (int)std::min(bound, (long)num_cus());      // as many workgroups as are resident at once
   if (grid <= 0) return 0;
   hipLaunchKernelGGL(kern, dim3(grid), dim3(64 * S::NW), lds, st, a);
@@ -506,16 +517,9 @@ int launch_tile_mx_t(const MxArgs& a, hipStream_t st) {
 
 }  // namespace
 
-// Gate/up: tiles of 128 rows where most experts fit one (from the layer-wide mean, never from the block bounds): 60 experts,
-// H 2048, I 1408, of 48 rows 79 us and 97 in tiles of 256, of 100 rows 93 and 109, of 150 rows 140 and 119.  (Tiles of 64: of 48
-// rows 77.)
 int launch_tile_mx_gateup(const MxArgs& a, hipStream_t st) {
-  const bool half_last = a.Kdim % 128 != 0;
-  if (a.mean_rows + 1.5 * sqrt((double)a.mean_rows) <= 128.0)
-    return half_last ? launch_tile_mx_t<128, true, true>(a, st) : launch_tile_mx_t<128, true, false>(a, st);
-  return half_last ? launch_tile_mx_t<256, true, true>(a, st) : launch_tile_mx_t<256, true, false>(a, st);
+  return a.Kdim % 128 != 0 ? launch_tile_mx_t<true, true>(a, st) : launch_tile_mx_t<true, false>(a, st);
 }
-// Down: 256 rows always.  (The same experts, of 48 rows 49 us and 52 in tiles of 128, of 100 rows 64 and 63, of 150 rows 71 and 99.)
-int launch_tile_mx_down(const MxArgs& a, hipStream_t st) { return launch_tile_mx_t<256, false, false>(a, st); }
+int launch_tile_mx_down(const MxArgs& a, hipStream_t st) { return launch_tile_mx_t<false, false>(a, st); }
 
 }  // namespace moe
