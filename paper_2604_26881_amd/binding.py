@@ -440,6 +440,14 @@ def _at(t, dtype, shape, name: str, what: str, dev: int) -> Optional[int]:
     raise MoeError(f"{what}: {name} must be on the current GPU, it is on {t.device}")
 
 
+def _result(t, x, dtype, shape, name: str, what: str, dev: int):
+    """An output and its address: the caller's tensor, checked, or a new one beside x (which is contiguous)."""
+    if t is None:
+        t = torch.empty_like(x, dtype=dtype) if shape == x.shape else x.new_empty(shape, dtype=dtype)
+        return t, t.data_ptr()
+    return t, _at(t, dtype, shape, name, what, dev)
+
+
 def _scales_shape(shape):
     return (*shape[:-1], shape[-1] // 32)
 
@@ -461,12 +469,9 @@ def moe_quantize_mx(x, q=None, scales=None):
         raise MoeError(f"{what}: the last dimension must be a multiple of 64, got {H}")
     dev = _device(x, "x", what)
     x_p = _at(x, _BF16, shape, "x", what, dev)
-    if q is None:
-        q = torch.empty_like(x, dtype=_E4M3)
-    if scales is None:
-        scales = torch.empty(_scales_shape(shape), dtype=_E8M0, device=x.device)
-    rc = load().moe_quantize_mx(x_p, x.numel() // H, H, _at(q, _E4M3, shape, "q", what, dev),
-                                _at(scales, _E8M0, _scales_shape(shape), "scales", what, dev), torch._C._cuda_getCurrentRawStream(dev))
+    q, q_p = _result(q, x, _E4M3, shape, "q", what, dev)
+    scales, s_p = _result(scales, x, _E8M0, _scales_shape(shape), "scales", what, dev)
+    rc = load().moe_quantize_mx(x_p, x.numel() // H, H, q_p, s_p, torch._C._cuda_getCurrentRawStream(dev))
     if rc != 0:
         _check(rc, what)
     return q, scales
@@ -483,16 +488,11 @@ def moe_residual_norm_mx(x, y=None, weight=None, eps: float = 1e-6, sum=None, ou
     dev = _device(x, "x", what)
     y_p, w_p = _at(y, _BF16, shape, "y", what, dev), _at(weight, _BF16, (H,), "weight", what, dev)
     x_p = _at(x, _BF16, shape, "x", what, dev)
-    sum = (torch.empty_like(x) if sum is None else sum) if keep_sum else None
-    out = (torch.empty_like(x) if out is None else out) if keep_out else None
-    if quantize:
-        q = torch.empty_like(x, dtype=_E4M3) if q is None else q
-        scales = torch.empty((T, H // 32), dtype=_E8M0, device=x.device) if scales is None else scales
-    else:
-        q = scales = None
-    rc = load().moe_residual_norm_mx(x_p, y_p, w_p, T, H, eps, _at(sum, _BF16, shape, "sum", what, dev), _at(out, _BF16, shape, "out", what, dev),
-                                     _at(q, _E4M3, shape, "q", what, dev), _at(scales, _E8M0, (T, H // 32), "scales", what, dev),
-                                     torch._C._cuda_getCurrentRawStream(dev))
+    sum, sum_p = _result(sum, x, _BF16, shape, "sum", what, dev) if keep_sum else (None, None)
+    out, out_p = _result(out, x, _BF16, shape, "out", what, dev) if keep_out else (None, None)
+    q, q_p = _result(q, x, _E4M3, shape, "q", what, dev) if quantize else (None, None)
+    scales, s_p = _result(scales, x, _E8M0, (T, H // 32), "scales", what, dev) if quantize else (None, None)
+    rc = load().moe_residual_norm_mx(x_p, y_p, w_p, T, H, eps, sum_p, out_p, q_p, s_p, torch._C._cuda_getCurrentRawStream(dev))
     if rc != 0:
         _check(rc, what)
     return sum, out, q, scales
@@ -514,13 +514,10 @@ def moe_route_scored(x, Wr, balance, K: int, score: str = "softmax", groups: int
     dev = _device(x, "x", what)
     Wr_p, b_p = _at(Wr, _BF16, (E, H), "Wr", what, dev), _at(balance, _F32, (E,), "balance", what, dev)
     x_p = _at(x, _BF16, None, "x", what, dev)
-    if topk_ids is None:
-        topk_ids = torch.empty((T, K), dtype=_I32, device=x.device)
-    if topk_w is None:
-        topk_w = torch.empty((T, K), dtype=_F32, device=x.device)
+    topk_ids, ids_p = _result(topk_ids, x, _I32, (T, K), "topk_ids", what, dev)
+    topk_w, tw_p = _result(topk_w, x, _F32, (T, K), "topk_w", what, dev)
     rc = load().moe_route_scored(x_p, Wr_p, b_p, T, H, E, K, SCORES[score], groups, top_groups, group_best, 1 if renorm else 0, scale,
-                                 _at(topk_ids, _I32, (T, K), "topk_ids", what, dev), _at(topk_w, _F32, (T, K), "topk_w", what, dev),
-                                 torch._C._cuda_getCurrentRawStream(dev))
+                                 ids_p, tw_p, torch._C._cuda_getCurrentRawStream(dev))
     if rc != 0:
         _check(rc, what)
     return topk_ids, topk_w
