@@ -5,7 +5,7 @@
 //
 // A tile is up to 256 token rows of one expert by 256 weight rows (gate/up: 128 gate rows and the matching 128 up rows), eight
 // waves as 2 x 4, each on half of the token rows by 64 weight rows (a gate block of 32 and its up block).  Its height is whole
-// blocks of 64 rows.  (Tiles of at most 128 rows, with as many stages, were up to 4 % faster for experts of 50 to 200 rows, and
+// blocks of 64 rows.  (Tiles of at most 128 rows, with as many stages, were up to 6 % faster for experts of 50 to 120 rows, and
 // far slower for more.)
 //
 // The kernel is persistent: every wave forms the tiles of the experts in registers from the row bounds on the device and walks
@@ -165,7 +165,7 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
   // Scales: 16 bytes of a row are GS steps.  The last group of a row that is not whole groups starts earlier instead, so that it
   // ends with the row.
   auto group_start = [&](int k) { return min(k / S::GS * 16, kb32 - 16); };
-  int group_in = 0, group_out = 0;       // the next group to be requested goes to the first, the one that is read lies in the second of these buffers
+  int group_in = 0, group_out = 0;       // the buffers of the next group to be requested, and of the one that is read
   // before the copies of K step kt the scales, if a group begins there.  (The copy is not counted in the waits, which makes them
   // wait for one copy more than they must.)
   auto issue_scales = [&](int kt) {
