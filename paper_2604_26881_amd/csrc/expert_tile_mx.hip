@@ -142,8 +142,10 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
   const int slot = xcd_walk ? (int)(blockIdx.x >> 3) : 0;
   const int run = xcd_walk ? max(1, min(G >> 3, (Lend + 7) >> 3)) : 1;
   if (xcd_walk && slot >= run) return;
-  const int L0 = xcd_walk ? (int)(blockIdx.x & 7) * run + slot : (int)blockIdx.x, step = xcd_walk ? 8 * run : G;
-  const int its = L0 < Lend ? (Lend - L0 + step - 1) / step : 0;
+  // Rounds of `step` tiles, one for every workgroup; the last, not a whole one, begins at the workgroups that had the lower tiles
+  // of the rounds before.
+  const int step = xcd_walk ? 8 * run : G, mine = xcd_walk ? (int)(blockIdx.x & 7) * run + slot : (int)blockIdx.x;
+  const int rounds = (Lend + step - 1) / step;
   const bool back = xcd_walk && (blockIdx.x & 1) != 0;      // half of the XCDs begin with the low tiles
 
   struct Tile { int row0, rowEnd, eg, rows, tbv, n0; bool valid; };
@@ -183,9 +185,13 @@ __global__ __launch_bounds__(512, 2) void expert_tile_mx_kernel(MxArgs a) {
   int gathered[S::NLA + 1];
   auto find_tile = [&]() -> Tile {
     Tile t{};
-    if (it >= its) return t;
-    int at = L0 + (back ? its - 1 - it : it) * step, h = S::TB;
-    ++it;
+    int at, h = S::TB;
+    do {
+      if (it == rounds) return t;
+      const int r = back ? rounds - 1 - it : it;
+      at = r * step + (r == rounds - 1 ? step - 1 - mine : mine);
+      ++it;
+    } while (at >= Lend);
     int tiles = total[S::TB - 1];
 #pragma unroll
     for (int i = S::TB - 1; i >= 1; --i)
