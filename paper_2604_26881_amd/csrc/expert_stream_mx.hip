@@ -13,20 +13,21 @@
 // A workgroup is four waves that share 16 * WB weight rows (gate/up: half of them gate rows, half the matching up rows) and up
 // to 16 * MT token rows of one expert, and cut K into four parts of whole steps: with one token's experts there are few column
 // blocks, and four times the waves have four times the requests in flight.  A wave copies a step global -> LDS (whole
-// 128-byte lines), takes it into registers, and asks for the next into the same place before it multiplies.  One stage per wave
-// and no more: what keeps the memory busy is workgroups side by side, whose first and last steps overlap (60 experts, 8.5 rows
-// each on average, H 2048, I 1408, gate/up and down: two stages 72 + 46 us, one 60 + 34).  The four partial sums meet in LDS and
-// are added in the order of the parts.  The cut depends on the contraction alone, so a row's bits do not depend on the block cut.
+// 128-byte lines), takes it into registers, and asks for a later one into the same place before it multiplies.  One stage per
+// wave: what keeps the memory busy is workgroups side by side, whose first and last steps overlap (60 experts, 8.5 rows each on
+// average, H 2048, I 1408, gate/up and down: two stages 83 + 48 us, one 59 + 34); where there are no others, two.  The four
+// partial sums meet in LDS and are added in the order of the parts.  The cut depends on the contraction alone, so a row's bits
+// do not depend on the block cut.
 // Only the 1 KB pieces that hold token rows of the expert are copied (8 rows of 8 bits, 4 of bf16; for one row of bf16 four
 // pieces would be half as many bytes as the weights).
 // The first weights are requested before anything else; the scales of the rows (1/32 of the bytes) come next to them, once.
 //
 // The workgroups are column blocks by tiles of token rows of the experts that have any; a tile is found in registers
 // from the row bounds on the device (a wave holds all of them, four experts per lane): experts without rows cost no workgroup
-// (one token, 8 of 256 experts, H 4096, I 2048: 27 + 17 us; with a workgroup for every expert 39 + 28).
+// (one token, 8 of 256 experts, H 4096, I 2048: 24 + 13 us; with a workgroup for every expert 39 + 28).
 //
 // Measured, gate/up + down (the weights at the 5.06 TB/s of a large copy in brackets): H 2048, I 1408, one token's 4 experts
-// 8.9 + 5.7 us (4.7 + 2.4), 60 experts of 8.5 rows 58 + 32 (70 + 35); H 4096, I 2048, 160 experts of 1.6 rows 398 + 200
+// 8.9 + 5.3 us (4.7 + 2.4), 60 experts of 8.5 rows 58 + 32 (70 + 35); H 4096, I 2048, 160 experts of 1.6 rows 398 + 200
 // (547 + 274).  With many experts the weights come at 6 to 7 TB/s; with one token's experts what is left is the chain of
 // latencies: row bounds, sort, first lines, two more, the sum, the store.
 //
@@ -39,21 +40,22 @@
 namespace moe {
 namespace {
 
-template <int MT, int WB, bool GATEUP>
+template <int MT, int WB, bool GATEUP, int NST>
 struct StreamMxShape {
   static constexpr int WROWS = 16 * WB;
   static constexpr int ROWS = 16 * MT;                      // token rows of a workgroup
   static constexpr int XROW = GATEUP ? 128 : 256;           // bytes of a token row per step
   static constexpr int XPIECE = 1024 / XROW;                // token rows of a 1 KB copy
   static constexpr int STAGE = WROWS * 128 + ROWS * XROW;   // of one wave
+  static constexpr int RING = NST * STAGE;
   static constexpr int SROWS = WROWS + (GATEUP ? ROWS : 0); // rows with scales
   static constexpr int LDP = ROWS + 1;                      // partial sums: [WROWS][LDP], a padding word per row
   static_assert(STAGE >= WROWS * LDP * 4, "a wave's partial sums take the place of its stage");
 };
 
-template <int MT, int WB, bool GATEUP>
+template <int MT, int WB, bool GATEUP, int NST>
 __global__ __launch_bounds__(256) void expert_stream_mx_kernel(MxArgs a) {
-  using S = StreamMxShape<MT, WB, GATEUP>;
+  using S = StreamMxShape<MT, WB, GATEUP, NST>;
   extern __shared__ __align__(16) unsigned char smem[];
   constexpr int NPER = GATEUP ? S::WROWS / 2 : S::WROWS;    // output columns of a workgroup
   const int tid = threadIdx.x, lane = tid & 63;
@@ -106,9 +108,9 @@ __global__ __launch_bounds__(256) void expert_stream_mx_kernel(MxArgs a) {
   const size_t wrow = (size_t)eg * N + n0;
   const uint8_t* W0 = a.B0 + wrow * Kdim;                   // the first WROWS / 2 rows, and the others
   const uint8_t* W1 = GATEUP ? a.B1 + wrow * Kdim : W0 + (size_t)(S::WROWS / 2) * Kdim;
-  unsigned char* const stage = smem + wave * S::STAGE;
-  unsigned char* const scales = smem + 4 * S::STAGE;         // [SROWS][kb32]: the weight rows, then the token rows
-  const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem, lds0 = lds_base + (uint32_t)(wave * S::STAGE);
+  unsigned char* const ring = smem + wave * S::RING;
+  unsigned char* const scales = smem + 4 * S::RING;         // [SROWS][kb32]: the weight rows, then the token rows
+  const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem, lds0 = lds_base + (uint32_t)(wave * S::RING);
   // copies of weights: lane -> row lane/8 of an 8-row group, slot lane%8 holding chunk slot xor row%8
   const int crow = lane >> 3, cchunk = (lane & 7) ^ crow;
   uint32_t coffW[WB];
@@ -119,14 +121,15 @@ __global__ __launch_bounds__(256) void expert_stream_mx_kernel(MxArgs a) {
   auto xchunk = [&](int i) { return GATEUP ? cchunk : (lane & 15) ^ ((i * 4 + (lane >> 4)) & 15); };
   const int r16 = lane & 15, g = lane >> 4, swz = r16 & 7;
 
-  auto issue_weights = [&](int s) {
+  auto issue_weights = [&](int s, uint32_t slot) {
+    const uint32_t l = lds0 + slot * S::STAGE;
     const int k = step_of(s);
     const uint32_t back = half_last && k == nk - 1 && cchunk >= 4 ? 64u : 0u;     // the missing half from the half that is there
     const size_t kb = (size_t)k * 128;
 #pragma unroll
-    for (int i = 0; i < WB; ++i) copy_to_lds_16(W0 + kb, coffW[i] - back, lds0 + (uint32_t)i * 1024u, true);
+    for (int i = 0; i < WB; ++i) copy_to_lds_16(W0 + kb, coffW[i] - back, l + (uint32_t)i * 1024u, true);
 #pragma unroll
-    for (int i = 0; i < WB; ++i) copy_to_lds_16(W1 + kb, coffW[i] - back, lds0 + (uint32_t)(WB + i) * 1024u, true);
+    for (int i = 0; i < WB; ++i) copy_to_lds_16(W1 + kb, coffW[i] - back, l + (uint32_t)(WB + i) * 1024u, true);
   };
 
   f32x4 acc[WB][MT];
@@ -138,7 +141,8 @@ __global__ __launch_bounds__(256) void expert_stream_mx_kernel(MxArgs a) {
   auto walk = [&](auto xn_) {
     constexpr int XN = decltype(xn_)::value;                // 1 KB pieces of token rows
     constexpr int MTX = (XN * S::XPIECE + 15) / 16;         // tiles of 16 token rows
-    if (kn > 0) issue_weights(0);
+    constexpr int NI = 2 * WB + XN;                         // copies of a stage
+    for (int s = 0; s < min(kn, NST); ++s) issue_weights(s, (uint32_t)s);
     auto token_row = [&](int m) -> int {                    // rows past the end repeat the last row
       const int r = rb + m0 + min(m, rows - 1);
       return a.gather != nullptr ? a.gather[r] / a.gather_div : r;
@@ -146,13 +150,13 @@ __global__ __launch_bounds__(256) void expert_stream_mx_kernel(MxArgs a) {
     uint32_t coffX[XN];
 #pragma unroll
     for (int i = 0; i < XN; ++i) coffX[i] = (uint32_t)token_row(xrow(i)) * (uint32_t)(GATEUP ? Kdim : 2 * Kdim) + (uint32_t)xchunk(i) * 16u;
-    auto issue_tokens = [&](int s) {
+    auto issue_tokens = [&](int s, uint32_t slot) {
       const int k = step_of(s);
       const bool tail = half_last && k == nk - 1;
 #pragma unroll
       for (int i = 0; i < XN; ++i) {
         const uint32_t back = tail && xchunk(i) >= (GATEUP ? 4 : 8) ? (uint32_t)S::XROW / 2u : 0u;
-        copy_to_lds_16(a.A + (size_t)k * S::XROW, coffX[i] - back, lds0 + (uint32_t)(S::WROWS * 128 + i * 1024));
+        copy_to_lds_16(a.A + (size_t)k * S::XROW, coffX[i] - back, lds0 + slot * S::STAGE + (uint32_t)(S::WROWS * 128 + i * 1024));
       }
     };
     // scales of the weight rows: two contiguous runs of WROWS / 2 rows
@@ -160,7 +164,7 @@ __global__ __launch_bounds__(256) void expert_stream_mx_kernel(MxArgs a) {
       const uint8_t* S0 = a.B0s + wrow * kb32;
       const uint8_t* S1 = GATEUP ? a.B1s + wrow * kb32 : S0 + (size_t)(S::WROWS / 2) * kb32;
       const int run = S::WROWS / 2 * kb32;                  // a multiple of 16 bytes (kb32 is even, WROWS / 2 of 8)
-      const uint32_t l = lds_base + 4u * S::STAGE;
+      const uint32_t l = lds_base + 4u * S::RING;
       for (int i = wave * 64; i < run / 16; i += 256) {
         if (i + lane < run / 16) {
           copy_to_lds_16(S0, (uint32_t)(i + lane) * 16u, l + (uint32_t)i * 16u);
@@ -176,13 +180,15 @@ __global__ __launch_bounds__(256) void expert_stream_mx_kernel(MxArgs a) {
       }
       wait_lds_reads();                                     // (these writes)
     }
-    if (kn > 0) issue_tokens(0);
+    for (int s = 0; s < min(kn, NST); ++s) issue_tokens(s, (uint32_t)s);
     wait_copies_but<0>();
     __syncthreads();
 
+    uint32_t slot = 0;
     for (int s = 0; s < kn; ++s) {
       const int k = step_of(s);
       const bool tail = half_last && k == nk - 1;
+      const unsigned char* const stage = ring + slot * S::STAGE;
       const unsigned char* sw0 = scales + r16 * kb32;
       u32x4 w[WB][2], x[MTX][S::XROW / 64];
       int sw[WB][GATEUP ? 1 : 2], sx[MTX];
@@ -219,10 +225,11 @@ __global__ __launch_bounds__(256) void expert_stream_mx_kernel(MxArgs a) {
         for (int i = 0; i < S::XROW / 64; ++i) asm volatile("" : "+v"(x[mt][i]));
         if (GATEUP) asm volatile("" : "+v"(sx[mt]));
       }
-      if (s + 1 < kn) {
-        issue_weights(s + 1);
-        issue_tokens(s + 1);
+      if (s + NST < kn) {
+        issue_weights(s + NST, slot);
+        issue_tokens(s + NST, slot);
       }
+      slot = NST == 1 || slot + 1 == NST ? 0u : slot + 1u;
       if (tail) {                                           // zeros in the half that is not there, and any finite scale
         const u32x4 zero = {0u, 0u, 0u, 0u};
 #pragma unroll
@@ -256,7 +263,7 @@ __global__ __launch_bounds__(256) void expert_stream_mx_kernel(MxArgs a) {
               acc[b][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, as_bf16x8(x[mt][GATEUP ? 0 : i]), acc[b][mt], 0, 0, 0);
           }
       }
-      wait_copies_but<0>();
+      if (NST > 1 && s + NST < kn) wait_copies_but<(NST - 1) * NI>(); else wait_copies_but<0>();      // the next step has landed
     }
   };
   if (rows <= S::XPIECE) walk(std::integral_constant<int, 1>{});
@@ -266,7 +273,7 @@ __global__ __launch_bounds__(256) void expert_stream_mx_kernel(MxArgs a) {
 
   // The partial sums meet in LDS, in the stages.  Accumulator element j of block b, tile mt: weight row 16 b + 4 g + j, token row
   // 16 mt + lane % 16.
-  float* const part = reinterpret_cast<float*>(stage);
+  float* const part = reinterpret_cast<float*>(ring);
 #pragma unroll
   for (int b = 0; b < WB; ++b)
 #pragma unroll
@@ -276,7 +283,7 @@ __global__ __launch_bounds__(256) void expert_stream_mx_kernel(MxArgs a) {
   __syncthreads();
   auto total = [&](int row, int m) -> float {
     const float* p = reinterpret_cast<const float*>(smem) + row * S::LDP + m;
-    constexpr int next = S::STAGE / 4;
+    constexpr int next = S::RING / 4;
     return ((p[0] + p[next]) + p[2 * next]) + p[3 * next];
   };
   constexpr int CG = NPER / 4;                              // groups of four output columns
@@ -292,13 +299,13 @@ __global__ __launch_bounds__(256) void expert_stream_mx_kernel(MxArgs a) {
   }
 }
 
-template <int MT, int WB, bool GATEUP>
+template <int MT, int WB, bool GATEUP, int NST>
 int launch_stream_mx_t(const MxArgs& a, hipStream_t st) {
-  using S = StreamMxShape<MT, WB, GATEUP>;
-  auto kern = expert_stream_mx_kernel<MT, WB, GATEUP>;
+  using S = StreamMxShape<MT, WB, GATEUP, NST>;
+  auto kern = expert_stream_mx_kernel<MT, WB, GATEUP, NST>;
   constexpr int lds_max = 160 * 1024;
-  static_assert(4 * S::STAGE + S::SROWS * (MX_DIM_MAX / MX) <= lds_max, "the longest contraction's scales fit beside the stages");
-  const int lds = 4 * S::STAGE + S::SROWS * (a.Kdim / MX);
+  static_assert(4 * S::RING + S::SROWS * (MX_DIM_MAX / MX) <= lds_max, "the longest contraction's scales fit beside the stages");
+  const int lds = 4 * S::RING + S::SROWS * (a.Kdim / MX);
   static std::atomic<uint64_t> lds_raised{0};
   const int nexp = a.hi - a.lo;
   if (nexp > 256) return -2;
@@ -313,13 +320,14 @@ template <bool GATEUP>
 int launch_stream_mx(const MxArgs& a, hipStream_t st) {
   // 32 token rows per workgroup where many experts have more than 16: 60 experts (H 2048, I 1408) of 12 rows 68 + 38 us, with
   // 16 rows 66 + 36; of 17 rows 72 + 42, with 16 rows 88 + 45.
-  if (a.mean_rows > 12) return launch_stream_mx_t<2, 4, GATEUP>(a, st);
-  // Down with so few blocks of 64 columns that compute units would have none: blocks of 32 (one token's 4 experts, H 2048: 5.7 us,
-  // with 64 columns 6.5; of four tokens' 15 experts both take 12).
-  if constexpr (!GATEUP) {
-    if ((long)std::min(a.hi - a.lo, a.rows_total) * (a.N / 64) < 256) return launch_stream_mx_t<1, 2, false>(a, st);
-  }
-  return launch_stream_mx_t<1, 4, GATEUP>(a, st);
+  if (a.mean_rows > 12) return launch_stream_mx_t<2, 4, GATEUP, 1>(a, st);
+  // Few workgroups, one to a compute unit: a second stage per wave, and for down, whose blocks are the longer ones, blocks of 32
+  // columns (H 2048, I 1408: one token's 4 experts 13.2 us both, with one stage 14.2, with that and 64 columns 15; two tokens' 8
+  // experts, down alone, 6.5 and 7.4; two of 8 experts, H 4096, I 7168, down alone, 12 and 16.  With 660 and 480 workgroups, 15
+  // experts, 19 + 12 with one stage, 24 + 14 with two.)
+  if ((long)std::min(a.hi - a.lo, a.rows_total) * (a.N / (GATEUP ? 32 : 64)) <= 256)
+    return launch_stream_mx_t<1, GATEUP ? 4 : 2, GATEUP, 2>(a, st);
+  return launch_stream_mx_t<1, 4, GATEUP, 1>(a, st);
 }
 
 }  // namespace

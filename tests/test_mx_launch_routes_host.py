@@ -58,24 +58,25 @@ TILES = {"gate/up": "expert_tile_mx_kernel<1,0>", "half": "expert_tile_mx_kernel
 
 
 @pytest.mark.parametrize("P,H,E,I,want", [
-    (4, 2048, 60, 1408, [STREAM + "<1,4,1>", STREAM + "<1,2,0>"]),                    # few blocks of columns: narrower ones for down
-    (8, 2048, 60, 1408, [STREAM + "<1,4,1>", STREAM + "<1,4,0>"]),
-    (720, 2048, 60, 1408, [STREAM + "<1,4,1>", STREAM + "<1,4,0>"]),                  # 12 rows per expert
-    (721, 2048, 60, 1408, [STREAM + "<2,4,1>", STREAM + "<2,4,0>"]),
-    (1440, 2048, 60, 1408, [STREAM + "<2,4,1>", STREAM + "<2,4,0>"]),                 # 24
+    (4, 2048, 60, 1408, [STREAM + "<1,4,1,2>", STREAM + "<1,2,0,2>"]),                # few workgroups: two stages, narrower blocks for down
+    (8, 2048, 60, 1408, [STREAM + "<1,4,1,1>", STREAM + "<1,2,0,2>"]),
+    (9, 2048, 60, 1408, [STREAM + "<1,4,1,1>", STREAM + "<1,4,0,1>"]),
+    (720, 2048, 60, 1408, [STREAM + "<1,4,1,1>", STREAM + "<1,4,0,1>"]),              # 12 rows per expert
+    (721, 2048, 60, 1408, [STREAM + "<2,4,1,1>", STREAM + "<2,4,0,1>"]),
+    (1440, 2048, 60, 1408, [STREAM + "<2,4,1,1>", STREAM + "<2,4,0,1>"]),             # 24
     (1441, 2048, 60, 1408, [TILES["gate/up"], TILES["down"]]),
     (1441, 2112, 60, 1408, [TILES["half"], TILES["down"]]),                           # a contraction of half steps
-    (9000, 448, 60, 1408, [STREAM + "<2,4,1>", TILES["down"]]),                       # contractions too short for tiles
-    (9000, 512, 60, 448, [TILES["gate/up"], STREAM + "<2,4,0>"]),
+    (9000, 448, 60, 1408, [STREAM + "<2,4,1,1>", TILES["down"]]),                       # contractions too short for tiles
+    (9000, 512, 60, 448, [TILES["gate/up"], STREAM + "<2,4,0,1>"]),
     (65536, 2048, 60, 1408, [TILES["gate/up"], TILES["down"]]),
 ])
 def test_kernels_of_the_expert_blocks(run, P, H, E, I, want):
     (rc, launches), = run([experts(P, H, E, I)])
     assert rc == 0 and [n for n, _ in launches] == want
     in_bounds(launches)
-    # the block cut changes no kernel that changes bits: only the width of down's blocks of columns goes by the block
+    # the block cut changes no kernel that changes bits: only the stages, and the width of down's blocks of columns, go by the block
     (rc, launches), = run([experts(P, H, E, I, 7, 11)])
-    same = lambda names: [n.replace("<1,2,0>", "<1,4,0>") for n in names]
+    same = lambda names: [n.replace("<1,2,0,2>", "<1,4,0,1>").replace("<1,4,1,2>", "<1,4,1,1>") for n in names]
     assert rc == 0 and same([n for n, _ in launches]) == same(want)
 
 
