@@ -285,7 +285,7 @@ def test_expert_rows_every_element(moe, counts, H, I):
         assert torch.equal(bits(part[lo:hi]), bits(Yp[lo:hi])) and bool((part[:lo] == 768).all()) and bool((part[hi:] == 768).all())
 
 
-@pytest.mark.parametrize("T,H,E,K,I", [(1, 128, 8, 2, 64), (33, 320, 16, 4, 192), (200, 512, 12, 3, 448), (700, 256, 4, 2, 320)])
+@pytest.mark.parametrize("T,H,E,K,I", [(1, 128, 8, 2, 64), (33, 320, 16, 4, 192), (200, 512, 12, 3, 448), (700, 256, 4, 2, 320), (1500, 512, 20, 2, 2048)])
 def test_rows_read_through_the_sort_equal_the_permuted_copy(moe, T, H, E, K, I):
     print(f"[case] gather T={T} H={H} E={E} K={K} I={I}", flush=True)
     g = torch.Generator().manual_seed(T)
@@ -408,8 +408,9 @@ def test_layer_in_8_bits(moe, T):
     assert bool((d <= 2.0 ** -8 * want.abs() + 8 * 2.0 ** -24 * (Yp[row].abs() * tw[..., None].abs()).sum(1) + 1e-30).all())
 
 
-def test_captured_layer_replays_like_the_eager_one_on_another_stream(moe):
-    s = layer_state(moe, 150, 256, 16, 4, 192, 3)
+@pytest.mark.parametrize("T,H,I", [(1, 512, 320), (150, 256, 192), (300, 1024, 1600)])     # streamed, and in tiles
+def test_captured_layer_replays_like_the_eager_one_on_another_stream(moe, T, H, I):
+    s = layer_state(moe, T, H, 16, 4, I, 3)
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
@@ -419,7 +420,7 @@ def test_captured_layer_replays_like_the_eager_one_on_another_stream(moe):
     with torch.cuda.graph(graph):
         layer(moe, s)
     for k in range(4):
-        s["x"].copy_(rows(150, 256, 50 + k).cuda())
+        s["x"].copy_(rows(T, H, 50 + k).cuda())
         layer(moe, s)
         torch.cuda.synchronize()
         want = {n: s[n].clone() for n in ("sum", "out", "ids", "Yp", "res")}
@@ -478,9 +479,14 @@ def test_route_scored_large_batches_and_many_groups(moe, T, H, E, K, score, grou
     check_route(moe, x, Wr, b, K, score, groups, top, best, True, 1.0)
 
 
+HEIGHTS = [300, 64, 65, 1, 0, 128, 192, 256, 257, 30, 90, 500, 20, 33, 127, 250, 5, 70, 64, 10]
 MORE_COUNTS = [  # mean rows of 13 to 24 (two tiles of 16), above 24, and hundreds; scale rows of odd numbers of pairs and of part groups
     ([24, 24, 13, 30, 2, 0], 704, 832), ([33, 15, 1, 17, 32, 31, 0, 16], 2048, 1408), ([40, 63, 100, 129, 1, 0, 7], 576, 704),
     ([40, 63, 100, 129, 1, 0, 7], 640, 576), ([300, 280, 260, 0], 1152, 1216), ([129, 200, 33, 0, 256, 257], 1600, 512), ([26], 4160, 2112),
+    # more workgroups than compute units, few rows each: one row, pieces of 4 and 8 rows that are full, begun or two
+    ([1] * 64, 512, 576), ([1, 0, 3, 4, 5, 8, 9, 16, 17, 12, 2, 7, 0, 13, 20, 33, 6, 1, 15, 10, 11, 14, 3, 8], 1088, 704), ([4, 8, 5, 1] * 10, 1024, 1408),
+    # tiles of every height, more than workgroups: several rounds of the walk, of gate/up and of down
+    (HEIGHTS, 512, 4096), (HEIGHTS, 4096, 576), (HEIGHTS, 3648, 1088),
 ]
 
 
