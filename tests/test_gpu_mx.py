@@ -487,6 +487,7 @@ MORE_COUNTS = [  # mean rows of 13 to 24 (two tiles of 16), above 24, and hundre
     ([1] * 64, 512, 576), ([1, 0, 3, 4, 5, 8, 9, 16, 17, 12, 2, 7, 0, 13, 20, 33, 6, 1, 15, 10, 11, 14, 3, 8], 1088, 704), ([4, 8, 5, 1] * 10, 1024, 1408),
     # tiles of every height, more than workgroups: several rounds of the walk, of gate/up and of down
     (HEIGHTS, 512, 4096), (HEIGHTS, 4096, 576), (HEIGHTS, 3648, 1088),
+    ([40], 16384, 576), ([70, 3], 576, 16384),                 # the longest contractions in tiles
 ]
 
 
