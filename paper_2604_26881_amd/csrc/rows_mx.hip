@@ -72,7 +72,7 @@ __device__ __forceinline__ double fold_sum_f64(double a) {
 }
 
 // u = x + y; n = u / sqrt(mean(u^2) + eps) * weight.  One workgroup per token row, up to 4 x 8 values per lane (H <= 8192).
-// Each lane sums its squares in fp32, the lanes' sums meet in fp64, and 1 / sqrt is fp64 kept as the sum of two fp32: n is
+// The sum of squares is fp64 (no square of a bf16 overflows there), and 1 / sqrt is fp64 kept as the sum of two fp32: n is
 // then off by little more than its last rounding, and as few 8-bit values as can be land on the wrong side of a border.  (It
 // costs nothing: 16 384 rows of 2048, all outputs, 54 us both ways, 5.6 TB/s.)  sum and out are rounded once from fp32, and so
 // are the 8-bit rows (from n itself, not from out).
@@ -82,7 +82,7 @@ __global__ __launch_bounds__(256) void residual_norm_mx_kernel(const bf16_t* x, 
   const size_t t = blockIdx.x;
   __shared__ double s_part[4];
   float u[4][8];
-  float ss = 0.0f;
+  double ss = 0.0;
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
     const int c = threadIdx.x + 256 * r;
@@ -95,10 +95,10 @@ __global__ __launch_bounds__(256) void residual_norm_mx_kernel(const bf16_t* x, 
         for (int i = 0; i < 8; ++i) u[r][i] += v[i];
       }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) ss = __builtin_fmaf(u[r][i], u[r][i], ss);
+      for (int i = 0; i < 8; ++i) ss = __builtin_fma((double)u[r][i], (double)u[r][i], ss);
     }
   }
-  const double wave_total = fold_sum_f64((double)ss);
+  const double wave_total = fold_sum_f64(ss);
   if ((threadIdx.x & 63) == 0) s_part[threadIdx.x >> 6] = wave_total;
   __syncthreads();
   const double scale = 1.0 / sqrt(((s_part[0] + s_part[1]) + (s_part[2] + s_part[3])) / (double)H + (double)eps);

@@ -127,6 +127,13 @@ def test_norm_in_place_and_rows_of_zeros_and_nan(moe):
     assert bool(torch.isnan(v[192:224]).all()) and not bool(torch.isnan(v[:192]).any()) and not bool(torch.isnan(v[224:]).any())
 
 
+@pytest.mark.parametrize("exponent,eps", [(100, 1e-6), (118, 0.0), (-40, 0.0), (-100, 0.0), (-100, 1e-6)])
+def test_norm_of_rows_whose_squares_leave_fp32(moe, exponent, eps):
+    x = (rows(9, 320, 17).double() * 2.0 ** exponent).to(torch.bfloat16)
+    y = (rows(9, 320, 18).double() * 2.0 ** exponent).to(torch.bfloat16)
+    check_norm(moe, x, y, rows(1, 320, 19)[0], eps)
+
+
 # ---- gating
 
 ROUTE = [  # T, H, E, K, score, groups, top_groups, best, renorm, scale, balance
