@@ -16,8 +16,8 @@
 // 128-byte lines), takes it into registers, and asks for a later one into the same place before it multiplies.  One stage per
 // wave: what keeps the memory busy is workgroups side by side, whose first and last steps overlap (60 experts, 8.5 rows each on
 // average, H 2048, I 1408, gate/up and down: two stages 83 + 48 us, one 59 + 34); where there are no others, two.  The four
-// partial sums meet in LDS and are added in the order of the parts.  The cut depends on the contraction alone, so a row's bits
-// do not depend on the block cut.
+// partial sums meet in LDS and are added in the order of the parts.  The parts depend on the contraction alone, and where a wave
+// starts in its part on the output column and the expert alone, so a row's bits do not depend on the block cut.
 // Only the 1 KB pieces that hold token rows of the expert are copied (8 rows of 8 bits, 4 of bf16; for one row of bf16 four
 // pieces would be half as many bytes as the weights).
 // The first weights are requested before anything else; the scales of the rows (1/32 of the bytes) come next to them, once.
@@ -50,6 +50,8 @@ struct StreamMxShape {
   static constexpr int RING = NST * STAGE;
   static constexpr int SROWS = WROWS + (GATEUP ? ROWS : 0); // rows with scales
   static constexpr int LDP = ROWS + 1;                      // partial sums: [WROWS][LDP], a padding word per row
+  static constexpr int START = GATEUP ? 32 : 64;            // output columns that share their start in K, in every form
+  static_assert(START % (GATEUP ? WROWS / 2 : WROWS) == 0, "a workgroup has one start");
   static_assert(STAGE >= WROWS * LDP * 4, "a wave's partial sums take the place of its stage");
 };
 
@@ -100,9 +102,10 @@ __global__ __launch_bounds__(256) void expert_stream_mx_kernel(MxArgs a) {
   const int nk = (Kdim + 127) / 128;
   const bool half_last = (Kdim & 127) != 0;
   // this wave's part of K: steps [k0, k0 + kn); its walk starts at a step of its own and wraps around (waves that start
-  // together would otherwise ask the same memory channels, see expert_stream_lds.hip)
+  // together would otherwise ask the same memory channels, see expert_stream_lds.hip).  The start goes by the output columns in
+  // units that every form has, never by the block of columns: how wide that is depends on the block cut (launch_stream_mx).
   const int k0 = nk * wave / 4, kn = nk * (wave + 1) / 4 - k0;
-  const int rot = kn > 0 ? (int)((column * 3u + (unsigned)eg * 5u) % (unsigned)kn) : 0;
+  const int rot = kn > 0 ? (int)(((unsigned)n0 / S::START * 3u + (unsigned)eg * 5u) % (unsigned)kn) : 0;
   auto step_of = [&](int s) { return k0 + (s + rot >= kn ? s + rot - kn : s + rot); };
 
   const size_t wrow = (size_t)eg * N + n0;
