@@ -72,10 +72,12 @@ __device__ __forceinline__ double fold_sum_f64(double a) {
 }
 
 // u = x + y; n = u / sqrt(mean(u^2) + eps) * weight.  One workgroup per token row, up to 4 x 8 values per lane (H <= 8192).
-// The sum of squares is fp64 (no square of a bf16 overflows there), and 1 / sqrt is fp64 kept as the sum of two fp32: n is
-// then off by little more than its last rounding, and as few 8-bit values as can be land on the wrong side of a border.  (It
-// costs nothing: 16 384 rows of 2048, all outputs, 54 us both ways, 5.6 TB/s.)  sum and out are rounded once from fp32, and so
-// are the 8-bit rows (from n itself, not from out).
+// The sum of squares is fp64 (no square of a bf16 overflows there), and so are 1 / sqrt and its products with u and the weight,
+// rounded once to fp32: n is the nearest fp32 wherever it is one, though 1 / sqrt alone may lie beyond the range of fp32 (eps 0
+// and rows of subnormals, large weights), and as few 8-bit values as can be land on the wrong side of a border.  sum and out
+// are rounded once from fp32, and so are the 8-bit rows (from n itself, not from out).  What bounds it is the bytes: 16 384 rows
+// of 2048, all outputs, 55 us, 5.5 TB/s; 777 rows of 4096, 8-bit rows alone, 4.8 us (with the factor as the sum of two fp32, which
+// overflowed, 55 and 4.6).
 __global__ __launch_bounds__(256) void residual_norm_mx_kernel(const bf16_t* x, const bf16_t* y, const bf16_t* __restrict__ weight,
                                                                int H, float eps, bf16_t* sum, bf16_t* out,
                                                                uint8_t* __restrict__ q, uint8_t* __restrict__ scales) {
@@ -102,7 +104,6 @@ __global__ __launch_bounds__(256) void residual_norm_mx_kernel(const bf16_t* x, 
   if ((threadIdx.x & 63) == 0) s_part[threadIdx.x >> 6] = wave_total;
   __syncthreads();
   const double scale = 1.0 / sqrt(((s_part[0] + s_part[1]) + (s_part[2] + s_part[3])) / (double)H + (double)eps);
-  const float scale_hi = (float)scale, scale_lo = (float)(scale - (double)scale_hi);
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
     const int c = threadIdx.x + 256 * r;
@@ -113,10 +114,7 @@ __global__ __launch_bounds__(256) void residual_norm_mx_kernel(const bf16_t* x, 
       float n[8], v[8] = {1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f};
       if (weight != nullptr) widen(reinterpret_cast<const u32x4*>(weight)[c], v);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float f = scale_hi * v[i], rest = __builtin_fmaf(scale_hi, v[i], -f) + scale_lo * v[i];
-        n[i] = __builtin_fmaf(u[r][i], f, u[r][i] * rest);
-      }
+      for (int i = 0; i < 8; ++i) n[i] = (float)((double)u[r][i] * (scale * (double)v[i]));
       if (out != nullptr)
         reinterpret_cast<u32x4*>(out + t * H)[c] = u32x4{pack_bf16x2(n[0], n[1]), pack_bf16x2(n[2], n[3]),
                                                          pack_bf16x2(n[4], n[5]), pack_bf16x2(n[6], n[7])};
