@@ -11,25 +11,23 @@
 // but add up in another order, and ids must not depend on that.  So: logits from the matrix cores with a bound of their
 // error, the choice from those; and where two candidates lie closer than the bound allows, the logits of just these are formed
 // again in the defined order (and their scores in 64 bits) and the choice is repeated: an id is always the definition's.
-// (Weights come from the logits at hand, whose last bits are either evaluation's.)  About one token in forty is looked at
+// (Weights come from the logits at hand, whose last bits are either evaluation's.)  About one token in eighteen is looked at
 // twice (256 experts in 8 groups, H 2048).
 //
 // Measured (H 2048): 13 tokens, 60 experts 9.4 us, 3 of them the products and 4 the choice; 301 tokens, 256 experts in 8 groups
 // 29 us (8 products: every workgroup reads the router's 1 MB; 2.5 their sum; 7 the choice, and 9 more where near ties are
 // formed again); 8192 such tokens 49 us (15 + 5 + 9, and up to 17); 16 384 tokens, 60 experts, sigmoid 33 us.
 //
-// The bound: one 16x16x32 step is off by at most 6 * 2^-24 of the sum of its terms' magnitudes (measured, products over 18
-// orders of magnitude among them), whole logits of H 2048 by 1.3 * 2^-24 of theirs, and the defined order by less; assumed
-// are 32 * 2^-24 (beyond H 2048 H / 64 * 2^-24) of |x[t]| * max_e |Wr[e]|, which is more than that sum.
+// The bound of the error is derived in score_margin.h from how often a term is rounded in either order, up to some 60 times
+// (H 2048), and so does not rest on how large errors usually are (1.3 * 2^-24 of the magnitudes' sum).
 #include "fold.h"
 #include "mx.h"
+#include "score_margin.h"
 #include <algorithm>
 #include <type_traits>
 
 namespace moe {
 namespace {
-
-constexpr float LOGIT_ERROR = 32.0f / 16777216.0f;
 
 // Whole numbers that order like the values: -0 as +0, NaN as 1, below -infinity; 0 is left for "no expert"
 __device__ __forceinline__ uint32_t order_key(float v) {
@@ -120,6 +118,7 @@ __device__ __forceinline__ bool choose(const RouteScored& a, int t, bool want, b
   const bool grouped = a.groups > a.top_groups;
   // softmax without extras orders like its logits
   const bool by_logit = !whole && !a.sigmoid && a.balance == nullptr && (!grouped || a.best == 1);
+  const bool by_score = !a.sigmoid && !by_logit;
   auto row_any = [&](bool v) { return ((__ballot(v) >> row0) & ((1ull << LANES) - 1ull)) != 0ull; };
 
   // Sum over the experts, in an order that does not depend on LANES: rows of 16 lanes add what rows of 32 have in two lanes as
@@ -137,7 +136,7 @@ __device__ __forceinline__ bool choose(const RouteScored& a, int t, bool want, b
   };
 
   uint32_t key[EPL];         // what is compared, 0 beyond E
-  float m = 0.0f, share = 0.0f;
+  float m = 0.0f;
   double z = 1.0;
   unsigned exact = whole ? ~0u : 0u;       // this lane's experts whose logit (and key) is the defined one
   bool redo = false;
@@ -152,7 +151,8 @@ __device__ __forceinline__ bool choose(const RouteScored& a, int t, bool want, b
     float magnitudes = 0.0f;
 #pragma unroll
     for (int i = 0; i < EPL; ++i) magnitudes += fabsf(l[i]);
-    if (row_any(magnitudes != 0.0f)) redo = !whole && (doubt < 0.0f || row_any(!(magnitudes < INFINITY)));
+    if (row_any(magnitudes != 0.0f))
+      redo = !whole && (doubt < 0.0f || (by_score && doubt > LOGIT_ERROR_MOST) || row_any(!(magnitudes < INFINITY)));
     else doubt = 0.0f;       // (a row of zeros: 0 in any order)
     if (!a.sigmoid) {
       float top = -INFINITY;
@@ -191,7 +191,6 @@ __device__ __forceinline__ bool choose(const RouteScored& a, int t, bool want, b
       for (int i = 0; i < EPL; ++i) l[i] = e0 + i < a.E ? expf(l[i] - m) : 0.0f;
       const float sum = sum_of(l);
       z = sum;
-      share = 2.1f * doubt + 4e-6f;
       const float inverse = 1.0f / sum;
 #pragma unroll
       for (int i = 0; i < EPL; ++i) l[i] *= inverse;
@@ -207,12 +206,7 @@ __device__ __forceinline__ bool choose(const RouteScored& a, int t, bool want, b
 #pragma unroll
     for (int i = 0; i < EPL; ++i) key[i] = e0 + i < a.E ? order_key(l[i]) : 0u;
   }
-  // what a compared value of magnitude c may be off by
-  const float own = a.sigmoid ? 0.25f * doubt + 2e-6f : by_logit ? doubt : 0.0f, largest = 1.0f / (float)z;
-  auto off = [&](float c) {
-    const float rounded = 2.4e-7f * c;
-    return a.sigmoid || by_logit ? own + rounded : share * fminf(largest, c + bal_most) + rounded + 1e-37f;
-  };
+  const ScoreMargin margin = a.sigmoid ? margin_of_sigmoids(doubt) : by_logit ? margin_of_logits(doubt) : margin_of_softmax(doubt, 1.0f / (float)z, bal_most);
   int my_id = 0;
   for (;;) {
     unsigned again = 0u;     // this lane's experts whose logit the choice needs exactly
@@ -284,7 +278,7 @@ __device__ __forceinline__ bool choose(const RouteScored& a, int t, bool want, b
 #pragma unroll
       for (int gi = 0; gi < GPL; ++gi) {
         const float v = key_value(value[gi]);
-        const float moved = 2.0f * a.best * off(0.5f * size_of[gi]) + 1e-6f * size_of[gi];      // two values, of one or two c each
+        const float moved = margin.between_groups(a.best, size_of[gi]);
         const bool in = !whole && value[gi] != 0u && size_of[gi] < INFINITY && vk - vn <= moved && v >= vk - moved && v <= vn + moved;
         thr[gi] = in ? low[gi] - moved : INFINITY;
         close |= in;
@@ -342,7 +336,7 @@ __device__ __forceinline__ bool choose(const RouteScored& a, int t, bool want, b
       };
       const float after = following(my_c, next), d = my_c - after, large = fmaxf(fabsf(my_c), fabsf(after));
       const bool both = (jl < a.K - 1 || (jl == a.K - 1 && border != 0u)) && large < INFINITY;
-      close = both && d <= 2.0f * off(large);
+      close = both && d <= 2.0f * margin.off(large);
       most = row_max<LANES>(fmaxf(jl < a.K && fabsf(my_c) < INFINITY ? fabsf(my_c) : 0.0f, fabsf(next) < INFINITY ? fabsf(next) : 0.0f));
       if (by_logit) {
         alike |= (both && d > 0.0f && d <= 4e-7f * fmaxf(1.0f, large)) || (jl < a.K && my_c - m < -70.0f);
@@ -358,7 +352,7 @@ __device__ __forceinline__ bool choose(const RouteScored& a, int t, bool want, b
     }
     close = !whole && row_any(close);
     if (__any(close)) {      // whose logits lie that near to another's, at or above the border of the choice
-      const float width = 2.0f * off(most);
+      const float width = 2.0f * margin.off(most);
       unsigned one = 0u, two = 0u;           // experts with a chosen value, or two, that near (a chosen one's own counts)
       for (int j = 0; j <= a.K; ++j) {
         const float c = j < a.K ? __shfl(my_c, row0 + j, WAVE) : next;
@@ -440,7 +434,8 @@ __device__ __forceinline__ bool choose(const RouteScored& a, int t, bool want, b
 // copies of 1 KB straight into the wave's own ring in LDS, whole lines with eight lanes side by side on a row, and come back
 // as operands from there.  (Loaded as operands, 16 rows by 16 bytes per 16 lanes, they took four times as long: 0.35 us per
 // block and wave, of the address unit.)  The eight partial sums meet in LDS, eight tiles at a time, and are added in the order
-// of the parts: a logit's bits depend on H alone.  The squares for the error bound are summed from the same operands.
+// of the parts: a logit's bits depend on H alone.  The squares for the error bound are summed from the same operands, weighted
+// by how often their terms are rounded.
 // The choice is a chain of small steps, bound by their latency: all eight waves share the tokens, 32 lanes for each of 16 (half as
 // many experts per lane as with 16 lanes: 301 tokens 29 us, with 16 lanes and half of the waves idle 33), 16 lanes for each of 32.
 constexpr int ROUTE_WAVES = 8, ROUTE_RING = 8;                               // items of 2 KB in a wave's ring
@@ -515,6 +510,7 @@ __global__ __launch_bounds__(64 * ROUTE_WAVES) void route_scored_kernel(RouteSco
     int slot = 0;
     u32x4 xa[TT][2];
     for (int k = k0; k < k1; ++k) {
+      const float roundings = (float)logit_roundings(k, k1, nk);
 #pragma unroll
       for (int j = 0; j < NQ; ++j) {
         wait_copies_but<2 * (AHEAD - 1)>();
@@ -527,10 +523,10 @@ __global__ __launch_bounds__(64 * ROUTE_WAVES) void route_scored_kernel(RouteSco
         if (j < TT) {
           xa[j < TT ? j : 0][0] = v0;
           xa[j < TT ? j : 0][1] = v1;
-          xn[j < TT ? j : 0] = squares(v1, squares(v0, xn[j < TT ? j : 0]));
+          xn[j < TT ? j : 0] = __builtin_fmaf(roundings, squares(v1, squares(v0, 0.0f)), xn[j < TT ? j : 0]);
         } else {
           const int b = j < TT ? 0 : j - TT;
-          wn[b] = squares(v1, squares(v0, wn[b]));
+          wn[b] = __builtin_fmaf(roundings, squares(v1, squares(v0, 0.0f)), wn[b]);
 #pragma unroll
           for (int tt = 0; tt < TT; ++tt) {
             acc[b][tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(v0), as_bf16x8(xa[tt][0]), acc[b][tt], 0, 0, 0);
@@ -578,9 +574,9 @@ __global__ __launch_bounds__(64 * ROUTE_WAVES) void route_scored_kernel(RouteSco
   }
   const int tk = (wave * 64 + lane) / S::LANES, t = t0 + tk;
   const float w2 = row_sum<16>(s_wn[r16] + s_wn[16 + r16]), x2 = row_sum<16>(s_xn[tk * 32 + r16] + s_xn[tk * 32 + 16 + r16]);
-  const bool known = x2 >= 1e-30f && x2 < INFINITY && w2 >= 1e-30f && w2 < INFINITY;     // (squares that did not vanish or overflow)
+  const bool known = x2 >= 1e-28f && x2 < INFINITY && w2 >= 1e-28f && w2 < INFINITY;     // (squares that did not vanish or overflow)
   uint32_t* const s_key = reinterpret_cast<uint32_t*>(smem) + tk * (S::EP + GROUPS_MAX);
-  const float doubt = known ? LOGIT_ERROR * fmaxf(1.0f, (float)H / 2048.0f) * sqrtf(x2) * sqrtf(w2) : -1.0f;
+  const float doubt = known ? LOGIT_ERROR_UNIT * sqrtf(x2) * sqrtf(w2) : -1.0f;
   int* const s_redo = reinterpret_cast<int*>(s_wn);                          // (every wave has read the norms before the barrier below)
   bool redo = false;
   for (int pass = 0; pass < 2; ++pass) {
