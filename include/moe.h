@@ -332,14 +332,15 @@ int moe_residual_norm_mx(const void* x, const void* y, const void* weight, int T
 
 /*
  * Gating by scores:
- *   logit as in moe_route (the same bits, without a bias) wherever the choice depends on them;
+ *   logit as in moe_route (the same bits, without a bias);
  *   s[t,e] = sigmoid(logit) or softmax over e (score), formed in 64 bits and rounded once to fp32;
  *   c[t,e] = s[t,e] + balance[e]  (fp32; balance [E] NULL: s): what the choice compares.  -infinity keeps an expert last;
  *   the experts form n_groups groups of E / n_groups neighbours, of which the top_groups with the largest value are kept: the
  *   value of a group is its largest c (group_best 1) or the sum of its two largest (2);
  *   topk_ids[t,:] = the K experts of the kept groups with the largest c, descending;
- *   topk_w[t,j] = s[t, topk_ids[t,j]], with renorm divided by (their sum over j + 1e-20), times scale (here the logits are fp32
- *                 sums in some order, the same for every batch).
+ *   topk_w[t,j] = s[t, topk_ids[t,j]], with renorm divided by (their sum over j + 1e-20), times scale.
+ * topk_ids are exactly these.  topk_w is formed in fp32 from logits that may be fp32 sums in another order (the same for every
+ * batch): it is off by what the logits differ by, and for equal logits by at most 2^-17 of itself.
  * Equal values go to the lower id (group or expert); NaN orders below everything else, so the ids of a row are K different
  * experts whatever it holds.  Row t of the outputs depends on row t of x only, bit for bit.
  *   1 <= n_groups <= 64 divides E; 1 <= top_groups <= n_groups; K <= top_groups * E / n_groups; group_best 1 or 2 and at most

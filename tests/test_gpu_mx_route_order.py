@@ -98,3 +98,21 @@ def test_logits_of_the_matrix_cores_are_within_the_bound_that_the_choice_counts_
     d = (got - exact).abs()
     assert bool((d <= 1.01 * u * bound + 2.0 ** -19)[sure].all()), float((d / (u * bound))[sure].max())
     print(f"largest error {float((d / (u * bound))[sure].max()):.3f} of the bound", flush=True)
+
+
+@pytest.mark.parametrize("T,H,E,K,score,groups,top,best,renorm,balance", [
+    (37, 512, 60, 4, "softmax", 1, 1, 1, False, False), (300, 2048, 256, 8, "sigmoid", 8, 4, 2, True, True),
+    (5000, 320, 256, 16, "softmax", 8, 3, 1, True, True), (64, 1088, 160, 6, "softmax", 4, 2, 2, False, True), (9, 64, 16, 16, "sigmoid", 1, 1, 1, False, False)])
+def test_weights_of_logits_that_any_order_adds_exactly(moe, T, H, E, K, score, groups, top, best, renorm, balance):
+    """Whole numbers times sixteenths: every partial sum is a float, so nothing is left but the scores.  In units of 2^-24: an
+    exponential 4 (two in the last place), the denominator 4 + 21 additions in a row, quotient and scale 1 each; with renorm the
+    denominator is common, and the chosen scores' sum is 5 + 15 additions: below 32 in all."""
+    print(f"[case] exact logits {T} {H} {E} {K} {score} {groups}", flush=True)
+    g = torch.Generator().manual_seed(T + H)
+    x = torch.randint(-2, 3, (T, H), generator=g).to(torch.bfloat16)
+    Wr = (torch.randint(-3, 4, (E, H), generator=g) * (torch.rand((E, H), generator=g) < 64.0 / H) / 16.0).to(torch.bfloat16)
+    b = torch.randint(-8, 9, (E,), generator=g) / (256.0 if score == "sigmoid" else 256.0 * E) if balance else None
+    ids, w = check_route(moe, x, Wr, b, K, score, groups, top, best, renorm, 2.5)
+    rid, rw = ref.route(x, Wr, b, K, score, groups, top, best, renorm, 2.5)
+    assert torch.equal(ids.cpu(), rid)
+    assert bool(((w - rw).abs() <= 2.0 ** -19 * rw.abs() + 1e-37).all()), float(((w - rw).abs() / rw.abs().clamp_min(1e-30)).max())
