@@ -40,7 +40,6 @@
 // at 1.8 GHz, the card's power limit, so fewer waits alone make it no faster: another barrier per step that let copies start
 // half a step earlier changed nothing.
 #include <algorithm>
-#include <type_traits>
 #include "fold.h"
 #include "mx.h"
 
@@ -77,8 +76,6 @@ struct TileMxShape {
 };
 constexpr int TILE_MX_MIN_K = 512;       // a row has 16 scale bytes
 
-template <int N>
-using number = std::integral_constant<int, N>;
 template <int FROM, int TO, class F>
 __device__ __forceinline__ void for_range(F&& f) {
   if constexpr (FROM < TO) {

@@ -8,8 +8,12 @@
 // multiplication by the inverse scale is exact, so the only rounding is the conversion's, to nearest even.
 #pragma once
 #include "common.h"
+#include <type_traits>
 
 namespace moe {
+
+template <int N>
+using number = std::integral_constant<int, N>;
 
 constexpr int MX = 32;                 // values per scale
 constexpr int MX_DIM_MAX = 16384;     // H and I of an expert block: the scales of a workgroup's rows fit LDS beside its rings

@@ -3,14 +3,11 @@
 // Both are streams: every input is read once, every output written once, the row stays in registers in between.  A lane
 // holds 8 neighbours (one 16-byte load, one 8-byte store), so the 32 values of a scale are the four lanes of a quad and
 // their maximum is two lane exchanges.
+#include "fold.h"
 #include "mx.h"
 #include <algorithm>
-#include <type_traits>
 
 namespace moe {
-
-template <int N>
-using number = std::integral_constant<int, N>;
 
 // Eight values of this lane, a quarter of a block: their bytes to q[0 .. 8), the scale by the quad's first lane to *scale
 __device__ __forceinline__ void store_mx8(const float (&v)[8], uint8_t* __restrict__ q, uint8_t* __restrict__ scale) {
@@ -25,10 +22,6 @@ __device__ __forceinline__ void store_mx8(const float (&v)[8], uint8_t* __restri
   *reinterpret_cast<uint2*>(q) = o;
   if ((threadIdx.x & 3) == 0) *scale = (uint8_t)byte;
 }
-__device__ __forceinline__ void widen(u32x4 v, float (&f)[8]) {
-  f[0] = bf16_lo(v.x); f[1] = bf16_hi(v.x); f[2] = bf16_lo(v.y); f[3] = bf16_hi(v.y);
-  f[4] = bf16_lo(v.z); f[5] = bf16_hi(v.z); f[6] = bf16_lo(v.w); f[7] = bf16_hi(v.w);
-}
 
 // n8: eighths, rows * H / 8 (the rows are contiguous, and H is whole blocks)
 __global__ __launch_bounds__(256) void quantize_mx_kernel(const bf16_t* __restrict__ x, size_t n8, uint8_t* __restrict__ q,
@@ -36,7 +29,7 @@ __global__ __launch_bounds__(256) void quantize_mx_kernel(const bf16_t* __restri
   const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= n8) return;     // (n8 is a multiple of 8: quads leave together)
   float v[8];
-  widen(reinterpret_cast<const u32x4*>(x)[i], v);
+  widen8(reinterpret_cast<const u32x4*>(x)[i], v);
   store_mx8(v, q + 8 * i, scales + i / 4);
 }
 
@@ -89,10 +82,10 @@ __global__ __launch_bounds__(256) void residual_norm_mx_kernel(const bf16_t* x, 
   for (int r = 0; r < 4; ++r) {
     const int c = threadIdx.x + 256 * r;
     if (c < H / 8) {
-      widen(reinterpret_cast<const u32x4*>(x + t * H)[c], u[r]);
+      widen8(reinterpret_cast<const u32x4*>(x + t * H)[c], u[r]);
       if (y != nullptr) {
         float v[8];
-        widen(reinterpret_cast<const u32x4*>(y + t * H)[c], v);
+        widen8(reinterpret_cast<const u32x4*>(y + t * H)[c], v);
 #pragma unroll
         for (int i = 0; i < 8; ++i) u[r][i] += v[i];
       }
@@ -112,7 +105,7 @@ __global__ __launch_bounds__(256) void residual_norm_mx_kernel(const bf16_t* x, 
         reinterpret_cast<u32x4*>(sum + t * H)[c] = u32x4{pack_bf16x2(u[r][0], u[r][1]), pack_bf16x2(u[r][2], u[r][3]),
                                                          pack_bf16x2(u[r][4], u[r][5]), pack_bf16x2(u[r][6], u[r][7])};
       float n[8], v[8] = {1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f};
-      if (weight != nullptr) widen(reinterpret_cast<const u32x4*>(weight)[c], v);
+      if (weight != nullptr) widen8(reinterpret_cast<const u32x4*>(weight)[c], v);
 #pragma unroll
       for (int i = 0; i < 8; ++i) n[i] = (float)((double)u[r][i] * (scale * (double)v[i]));
       if (out != nullptr)
