@@ -27,7 +27,7 @@
 // (one token, 8 of 256 experts, H 4096, I 2048: 24 + 13 us; with a workgroup for every expert 39 + 28).
 //
 // Measured, gate/up + down (the weights at the 5.06 TB/s of a large copy in brackets): H 2048, I 1408, one token's 4 experts
-// 8.9 + 5.3 us (4.7 + 2.4), 60 experts of 8.5 rows 58 + 32 (70 + 35); H 4096, I 2048, 160 experts of 1.6 rows 398 + 200
+// 8.3 + 5.2 us (4.7 + 2.4), 60 experts of 8.5 rows 58 + 33 (70 + 35); H 4096, I 2048, 160 experts of 1.6 rows 398 + 200
 // (547 + 274).  With many experts the weights come at 6 to 7 TB/s; with one token's experts what is left is the chain of
 // latencies: row bounds, sort, first lines, two more, the sum, the store.
 //

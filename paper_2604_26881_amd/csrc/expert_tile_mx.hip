@@ -15,7 +15,7 @@
 // of few rows strewn in, some workgroups had half again as much as others: 4096 tokens drawn by rank (E 60, H 2048, I 1408)
 // 173 + 152 us, this way 162 + 137; 2000 such tokens (E 128, H 1024, I 768) 66 + 72, 60 + 60.  With many rows everywhere the
 // order by expert was the better one, by the weights that an expert's last tile shares with its others: 16 384 tokens
-// 440 + 380 us, 463 + 381.
+// 440 + 380 us, 463 + 381.  (Builds that differed in the order alone, means of 20 passes on a card not yet warm.)
 //
 // K steps of 128 (gate/up) or 64 (down: a bf16 row has as many bytes) through a ring of LDS stages filled by asynchronous
 // copies, more of them the lower the tile, a row's 16-byte chunks xor-swizzled against bank conflicts; one barrier per step.
@@ -35,10 +35,10 @@
 // tile's height.
 //
 // Measured: one expert of 16 384 rows, H 8192, I 4096: gate/up 895 us, 2.46 PFLOP/s, down 805, 1.37.  16 384 tokens on 60
-// experts, H 2048, I 1408: 463 + 381 us; what is lost against the former's rates are the first and last steps of tiles of 16
-// and 22 steps, the sigmoid and the stores (65 us of gate/up), and 5 % to workgroups that wait for the last ones.  Gate/up runs
-// at 1.8 GHz, the card's power limit, so fewer waits alone make it no faster: another barrier per step that let copies start
-// half a step earlier changed nothing.
+// experts, H 2048, I 1408: 427 + 369 us, 4096 drawn by rank 154 + 130, the 2000 of E 128 73 + 65 (medians of 40 passes on a warm
+// card).  What is lost against the former's rates are the first and last steps of tiles of 16 and 22 steps, the sigmoid and the
+// stores (65 us of gate/up), and 5 % to workgroups that wait for the last ones.  Gate/up runs at 1.8 GHz, the card's power limit, so
+// fewer waits alone make it no faster: another barrier per step that let copies start half a step earlier changed nothing.
 #include <algorithm>
 #include "fold.h"
 #include "mx.h"

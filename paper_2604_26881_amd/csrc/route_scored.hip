@@ -15,9 +15,11 @@
 // what is lost in the difference to the largest logit, on top of the logits' own error.)  About one token in eighteen is looked at
 // twice (256 experts in 8 groups, H 2048).
 //
-// Measured (H 2048): 13 tokens, 60 experts 9.4 us, 3 of them the products and 4 the choice; 301 tokens, 256 experts in 8 groups
-// 29 us (8 products: every workgroup reads the router's 1 MB; 2.5 their sum; 7 the choice, and 9 more where near ties are
-// formed again); 8192 such tokens 49 us (15 + 5 + 9, and up to 17); 16 384 tokens, 60 experts, sigmoid 33 us.
+// Measured (H 2048): 13 tokens, 60 experts 8.6 us, 3 of them the products and 4 the choice; 301 tokens, 256 experts in 8 groups
+// 28.6 us (8 products: every workgroup reads the router's 1 MB; 2.5 their sum; 7 the choice, and 9 to 10 more where near ties are
+// formed again); 8192 such tokens 48.5 us (15 + 5 + 9, and up to 18); 16 384 tokens, 60 experts, sigmoid 32 us.  2000 tokens of 160
+// experts in 8 groups, softmax, H 4096: 33 us, with a balance 71 (best 1) and 75 (best 2): groups that are near to each other have
+// all of the token's logits formed again.
 //
 // The bound of the error is derived in score_margin.h from how often a term is rounded in either order, up to some 60 times
 // (H 2048), and so does not rest on how large errors usually are (1.3 * 2^-24 of the magnitudes' sum).
@@ -438,7 +440,7 @@ __device__ __forceinline__ bool choose(const RouteScored& a, int t, bool want, b
 // of the parts: a logit's bits depend on H alone.  The squares for the error bound are summed from the same operands, weighted
 // by how often their terms are rounded.
 // The choice is a chain of small steps, bound by their latency: all eight waves share the tokens, 32 lanes for each of 16 (half as
-// many experts per lane as with 16 lanes: 301 tokens 29 us, with 16 lanes and half of the waves idle 33), 16 lanes for each of 32.
+// many experts per lane as with 16 lanes: 301 tokens 4 us less than with 16 lanes and half of the waves idle), 16 lanes for each of 32.
 constexpr int ROUTE_WAVES = 8, ROUTE_RING = 8;                               // items of 2 KB in a wave's ring
 template <int NBLK, int TT>
 struct RouteShape {
