@@ -297,8 +297,14 @@ __device__ __forceinline__ bool choose(const RouteScored& a, int t, bool want, b
         }
         __builtin_amdgcn_wave_barrier();
       }
-      if (by_logit) alike = (vk != vn && vk - vn <= 2e-6f * fmaxf(1.0f, fabsf(vk))) || vk - m < -70.0f;
-      else if (!a.sigmoid) alike = close;
+      if (by_logit) {        // against the best value that differs: groups with the last one's own stand in their order already
+        uint32_t differs = 0u;
+#pragma unroll
+        for (int gi = 0; gi < GPL; ++gi) differs = left[gi] != last ? max(differs, left[gi]) : differs;
+        alike = vk - key_value(row_max<LANES>(differs)) <= 2e-6f * fmaxf(1.0f, fabsf(vk)) || vk - m < -70.0f;      // (none: NaN)
+      } else if (!a.sigmoid) {
+        alike = close;
+      }
 #pragma unroll
       for (int i = 0; i < EPL; ++i) cur[i] = (kept >> group_of(e0 + i)) & 1ull ? cur[i] : 0u;
     }
@@ -318,9 +324,9 @@ __device__ __forceinline__ bool choose(const RouteScored& a, int t, bool want, b
       for (int i = EPL - 1; i >= 0; --i) e = cur[i] == k ? (uint32_t)(e0 + i) : e;
       return (int)row_min<LANES>(e);
     };
-    uint32_t my_key = 0u;                    // lane j < K: the j-th choice
+    uint32_t my_key = 0u, last_key = 0u;     // lane j < K: the j-th choice
     for (int j = 0; j < a.K; ++j) {
-      const uint32_t k = best_left();
+      const uint32_t k = last_key = best_left();
       const int e = expert_of(k);
 #pragma unroll
       for (int i = 0; i < EPL; ++i) cur[i] = e == e0 + i ? 0u : cur[i];
@@ -341,8 +347,12 @@ __device__ __forceinline__ bool choose(const RouteScored& a, int t, bool want, b
       const bool both = (jl < a.K - 1 || (jl == a.K - 1 && border != 0u)) && large < INFINITY;
       close = both && d <= 2.0f * margin.off(large);
       most = row_max<LANES>(fmaxf(jl < a.K && fabsf(my_c) < INFINITY ? fabsf(my_c) : 0.0f, fabsf(next) < INFINITY ? fabsf(next) : 0.0f));
-      if (by_logit) {
-        alike |= (both && d > 0.0f && d <= 4e-7f * fmaxf(1.0f, large)) || (jl < a.K && my_c - m < -70.0f);
+      if (by_logit) {        // again the best one left whose value differs from the last choice's
+        uint32_t differs = 0u;
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) differs = cur[i] != last_key ? max(differs, cur[i]) : differs;
+        const float e = my_c - following(my_c, key_value(row_max<LANES>(differs)));
+        alike |= jl < a.K && ((e > 0.0f && e <= 4e-7f * fmaxf(1.0f, fabsf(my_c))) || my_c - m < -70.0f);
       } else if (!a.sigmoid) {               // between exact logits what is left is the denominator's error
         float score = my_c, score_next = next;
         if (a.balance != nullptr) {
